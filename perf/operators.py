@@ -449,6 +449,7 @@ def _run_accept(s):
         law = torch.where(rejected[:, None], rest, law)
     upto = torch.cumsum(law, -1)
     token = (upto <= (w.double() * upto[:, -1])[:, None]).sum(-1).clamp(max=V - 1)
+    token = torch.where(upto[:, -1] > 0, token, -1)                  # a law without a positive weight
     tokens = torch.where(j[None] < acc[:, None], dl, -1)
     tokens = torch.cat([tokens, tokens.new_full((R, 1), -1)], -1)
     tokens[r, acc] = token
