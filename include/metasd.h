@@ -326,6 +326,108 @@ int32_t metasd_sample_logits(const float* logits, int32_t rows, int32_t V, float
 int32_t metasd_philox_words(uint64_t seed, uint32_t c0_start, int32_t n, uint32_t c1, uint32_t c2, uint32_t c3,
                             uint32_t* out, void* hip_stream);
 
+/* ---- requests whose K and V lie in 4-bit pages ---------------------------------------------------------------------
+ * One verification step of a serving program for a batch of requests, each operator on device arrays of the caller's, asynchronous on
+ * hip_stream of the current device and free of allocations, so that a step can be captured into a graph:
+ *   metasd_page_plan    lengths -> block table, and the slot and position of every new row
+ *   metasd_rope_append  queries and keys rotated for their positions; K and V into their slots in 4 bits
+ *   metasd_attn_pages   every request's new rows attend to its pages
+ *   metasd_accept_probs drafted tokens verified against the target's probabilities with the caller's random numbers
+ * dtype: METASD_F32 or METASD_BF16, of the rows of q, k, v and outputs.  Rows are `ld` elements apart, the heads of a row next to each other;
+ * rows start on 16 bytes.
+ *
+ * 4-bit rows.  The head_dim values of a position and K/V head are held in blocks of 32: codes of one sign, two exponent and one mantissa
+ * bit (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; nearest, ties to the even code) times 2^e, one e per block: the smallest with
+ * amax <= 7 * 2^e, -125 <= e <= 125, held as the byte e + 127.  4.25 bits per value.  Where K or V of a position and head has an infinity or a
+ * NaN, the position is marked for that head: both read back as NaN, and so do the attention rows that see it.
+ * Page: `page` positions of every K/V head, [head][page / 16 tiles][17 head_dim bytes]; a tile is 16 positions of a head: K codes, V codes
+ * (8 head_dim bytes each), K scales, V scales (head_dim / 2 each).  With position p of the tile, a byte holding the dimensions (d, d + 1), the
+ * even one in its low half: K codes [(d % 32) / 8][p][d / 32][(d % 8) / 2], K scales [p][d / 32], V codes [p / 4][(d % 32) / 2][d / 32][p % 4],
+ * V scales [p / 4][d / 32][p % 4].  Slot s is position s % page of page s / page.  Several layers can share a table: a page then holds all of
+ * them, page_stride bytes apart, and pool points at the layer in hand. */
+typedef struct {
+    int32_t n_kv_heads, head_dim; /* head_dim 32, 64 or 128 */
+    int32_t page, n_pages;        /* positions of a page: a power of two from 16 to 1024; n_pages * page < 2^31 */
+    void* pool;                   /* device, 16-byte aligned */
+    size_t page_stride;           /* bytes from page to page, a multiple of 16, at least metasd_page_bytes */
+} metasd_pages;
+
+/* Bytes of one page (of one layer). */
+int32_t metasd_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page, size_t* bytes_out);
+
+/* Block tables and slots for the rows that requests are about to add.  Request b has lens[b] positions and adds n_new[b] (negative ones count
+ * as 0), for which it needs ceil((lens[b] + n_new[b]) / page) pages; it holds held[b], listed in table[b][0 .. held[b]).
+ *   - What it holds beyond its need (drafts that were rejected, a request that has ended: lens = n_new = 0) goes back.
+ *   - What it lacks is taken from the free pages, in the order of the requests.  Requests for which nothing is left, whose need exceeds
+ *     `width`, or whose rows do not fit into `rows`, are not served: served[b] = 0, no slots, nothing taken.
+ * Free pages are a ring of page numbers: state = {place of the first, how many, 0, 0}; pages are taken from the front and given back behind the
+ * last, and pages given back can be taken from the next call on.  All arrays are int32 on the device; table [batch][width], held [batch],
+ * ring [n_pages] and state [4] are updated in place (a new pool: held = 0, ring = 0 .. n_pages - 1, state = {0, n_pages, 0, 0}).
+ * Out: start [batch + 1], the first row of every request in a block of all new rows; slots [rows] and pos [rows], where each goes and its
+ * position (slot -1: request not served; both -1: behind the last row); served [batch]. */
+#define METASD_PLAN_MAX_BATCH 4096
+int32_t metasd_page_plan(int32_t* table, int32_t batch, int32_t width, int32_t* held, int32_t* ring, int32_t n_pages, int32_t* state,
+                         const int32_t* lens, const int32_t* n_new, int32_t page, int32_t rows, int32_t* slots, int32_t* pos, int32_t* start,
+                         int32_t* served, void* hip_stream);
+
+/* Rotary positions.  Of the first rot_dim components of a head, the pairs (x, y) = (i, i + rot_dim / 2) (HALF) or (2 i, 2 i + 1) (PAIRS)
+ * become gain * (x cos a - y sin a, y cos a + x sin a) with a = position * f_i; the rest passes through (rot_dim 0: everything does).
+ *   PLAIN   f_i = theta^(-2 i / rot_dim)
+ *   LINEAR  f_i / factor
+ *   WAVE    by the turns t = orig_ctx f_i / (2 pi) that a pair makes in the original context: s = clamp((t - low) / (high - low), 0, 1),
+ *           f_i (s + (1 - s) / factor)
+ *   INDEX   by the place of the pair: with i(t) = rot_dim ln(orig_ctx / (2 pi t)) / (2 ln theta), a = max(floor(i(high)), 0) and
+ *           b = min(ceil(i(low)), rot_dim - 1), s = clamp((i - a) / max(b - a, 0.001), 0, 1), f_i ((1 - s) + s / factor) */
+#define METASD_ROPE_HALF 0
+#define METASD_ROPE_PAIRS 1
+#define METASD_ROPE_PLAIN 0
+#define METASD_ROPE_LINEAR 1
+#define METASD_ROPE_WAVE 2
+#define METASD_ROPE_INDEX 3
+typedef struct {
+    int32_t style, rot_dim, scaling, orig_ctx;
+    float theta, factor, low, high, gain;
+} metasd_rope;
+
+/* Row r at position pos[r]: q rotated into q_out (which may be q itself), k rotated and v appended at slots[r] (slot -1, or outside the pool:
+ * nothing is appended; the slots of a call differ from each other).  q and q_out may be NULL (nothing to rotate), or k, v and slots (nothing
+ * to append; pages then only gives head_dim).  Angles are formed in 64 bits, the rotation in 32. */
+int32_t metasd_rope_append(const metasd_rope* rope, const metasd_pages* pages, int32_t dtype, int32_t rows, int32_t n_heads, const void* q,
+                           int64_t q_ld, void* q_out, int64_t q_out_ld, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
+                           const int32_t* pos, const int32_t* slots, void* hip_stream);
+
+/* The values that the codes at slots[r] stand for: k, v [rows][n_kv_heads][head_dim] (zeros where the slot is -1 or outside the pool). */
+int32_t metasd_kv_rows(const metasd_pages* pages, const int32_t* slots, int32_t rows, int32_t dtype, void* k, void* v, void* hip_stream);
+
+/* Attention: request b's rows are start[b] .. start[b + 1] - 1 of q [rows][n_heads][head_dim], the last start[b + 1] - start[b] of its lens[b]
+ * positions, which all lie in its pages; row i of n sees the positions up to lens[b] - n + i (a row that sees none becomes zeros).  Query head h
+ * reads K/V head h / (n_heads / n_kv_heads).  out = softmax(scale q K^T) V, rows behind the last request are left as they were.
+ * max_new: the most rows a request has (further ones are not computed), max_len: about the longest context; both only bound the launch,
+ * lengths are read on the device.  A table entry outside the pool is read as its last page.  bf16: weights are rounded to bf16 before the
+ * product with V; fp32: q and weights are taken as two bf16 terms, 16 bits; sums are in 32 bits.
+ * scratch: metasd_attn_pages_scratch bytes for the same arguments on the same device (may be 0: NULL), used by one call at a time. */
+int32_t metasd_attn_pages_scratch(int32_t batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t max_new,
+                                  int32_t max_len, size_t* bytes_out);
+int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows, int32_t n_heads, const void* q, int64_t q_ld, void* out,
+                          int64_t out_ld, const int32_t* table, int32_t batch, int32_t width, const int32_t* start, const int32_t* lens,
+                          int32_t max_new, int32_t max_len, float scale, void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/* Alg. 3 on probabilities (after whatever the caller does to its logits) with the caller's random numbers: request b has n_draft[b] drafts
+ * (NULL: gamma; clamped to 0 .. gamma) d[b][j].  Draft j is accepted if u[b][j] * q < p with p = P[b][j][d], q = Q[b][j][d]; Q == NULL: drafts
+ * without a law (copied from a text), q = 1 at the draft and 0 elsewhere.  n_acc[b] = the first failure (a draft outside the vocabulary
+ * fails), else n_draft[b].  The token after it is drawn by inverse CDF with w[b] - the smallest v whose sum of weights up to v exceeds w[b]
+ * times their sum - from max(0, P - Q) at the failure (P itself if that is zero everywhere), or from P[b][n_draft[b]]; -1 if no weight is
+ * positive.  Weights need not sum to one; what is not above zero, a NaN among them, counts as zero.  Sums are in 64 bits.
+ * P [rows][gamma + 1][V]: elements (b, j, v) at b * p_row + j * p_pos + v; Q the same; d [rows][gamma], u [rows][gamma], w [rows].
+ * Out: n_acc [rows], tokens [rows][gamma + 1]: the accepted drafts, the drawn token, -1 behind it.
+ * scratch: METASD_ACCEPT_PROBS_SCRATCH_BYTES, 16-byte aligned, used by one call at a time. */
+#define METASD_ACCEPT_PROBS_MAX_VOCAB (1 << 20)
+#define METASD_ACCEPT_PROBS_SEGMENT 4096
+#define METASD_ACCEPT_PROBS_SCRATCH_BYTES(rows, V) ((size_t)(rows) * (((size_t)(V) + METASD_ACCEPT_PROBS_SEGMENT - 1) / METASD_ACCEPT_PROBS_SEGMENT) * 16)
+int32_t metasd_accept_probs(const float* P, int64_t p_row, int64_t p_pos, const float* Q, int64_t q_row, int64_t q_pos, const int32_t* d,
+                            const int32_t* n_draft, const float* u, const float* w, int32_t rows, int32_t gamma, int32_t V, int32_t* n_acc,
+                            int32_t* tokens, void* scratch, void* hip_stream);
+
 /* ---- measurement aids: not part of the method's boundary (no step of Alg. 1-3 needs them); benchmarks use them to
  * state achieved bandwidth per kernel next to what the machine reaches on a plain read ------------------------- */
 

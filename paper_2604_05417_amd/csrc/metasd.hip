@@ -25,6 +25,7 @@
 #include "step.h"
 #include "step_f32.h"
 #include "chain_f32.h"
+#include "pages_host.h"
 
 using namespace msd;
 
@@ -34,9 +35,9 @@ using namespace msd;
 static __device__ __align__(256) unsigned char scratch[(size_t)METASD_ACCEPT_NOALLOC_MAX_ITEMS * 336];
 
 namespace {
-
 thread_local std::string g_err = "";
-
+}
+namespace msd {
 int fail_global(int code, const char* fmt, ...) {
     char buf[512];
     va_list ap;
@@ -46,6 +47,9 @@ int fail_global(int code, const char* fmt, ...) {
     g_err = buf;
     return code;
 }
+}  // namespace msd
+
+namespace {
 
 constexpr int PER_LAYER = 9;
 constexpr int MAX_ROWS = 16;

@@ -6,11 +6,6 @@ namespace msd {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// the two-term form of a pair: hi = bf16(x), lo = bf16(x - hi)
-__device__ __forceinline__ void split_pair(float a, float b, uint32_t& hi, uint32_t& lo) {
-    hi = f2bf2(a, b);
-    lo = f2bf2(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
-}
 // Transposing LDS read: the 16 lanes of a group give the addresses of a 4 x 16 block of 16-bit elements (lane i: row i / 4,
 // columns 4 (i % 4) .. + 3); lane i receives column i (rows 0 .. 3).
 __device__ __forceinline__ s16x4 lds_read_tr(const bf16_t* p) {
