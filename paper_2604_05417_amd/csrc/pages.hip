@@ -101,16 +101,15 @@ void launch_rope(const RopeArgs<T>& a, const RopeTab& rt, const Pool& pl, int n_
 template <int HD, int TERMS>
 void launch_attn(const PagesAttn& a, const Pool& pl, const PagesPlan& p, hipStream_t st) {
     const dim3 grid((unsigned)((size_t)a.B * pl.KH * a.nsp * a.ncg)), block(64 * PA_NW);
-    switch (p.ct) {
-        case 1: hipLaunchKernelGGL((attn_pages_kernel<HD, 1, TERMS>), grid, block, 0, st, a, pl); break;
-        case 2: hipLaunchKernelGGL((attn_pages_kernel<HD, 2, TERMS>), grid, block, 0, st, a, pl); break;
-        default:
-            if constexpr (TERMS == 1) hipLaunchKernelGGL((attn_pages_kernel<HD, 4, TERMS>), grid, block, 0, st, a, pl);
-    }
+#define GO(CT, PACK) hipLaunchKernelGGL((attn_pages_kernel<HD, CT, TERMS, PACK>), grid, block, 0, st, a, pl)
+    if (p.ct == 2) GO(2, 1);
+    else if (TERMS == 1 || p.pack == 1) GO(1, 1);
+    else if constexpr (TERMS > 1) { if (p.pack == 2) GO(1, 2); else GO(1, 4); }
+#undef GO
     if (a.nsp > 1) {
         constexpr int UN = 256 / (HD / 4);
         const size_t units = (size_t)a.B * a.max_new * a.H;
-        hipLaunchKernelGGL((pages_merge_kernel<HD, TERMS>), dim3((unsigned)((units + UN - 1) / UN)), dim3(256), 0, st, a, pl, p.ct);
+        hipLaunchKernelGGL((pages_merge_kernel<HD, TERMS>), dim3((unsigned)((units + UN - 1) / UN)), dim3(256), 0, st, a, pl, p.cols);
     }
 }
 
@@ -239,7 +238,7 @@ int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows
                       max_new, p.spw, p.nsp, p.ncg};
     const Pool pl = pool_of(*pages);
     hipStream_t st = (hipStream_t)hip_stream;
-#define GO(HD) if (dtype == METASD_BF16) launch_attn<HD, 1>(a, pl, p, st); else launch_attn<HD, 2>(a, pl, p, st)
+#define GO(HD) if (dtype == METASD_BF16) launch_attn<HD, 1>(a, pl, p, st); else launch_attn<HD, 3>(a, pl, p, st)
     if (hd == 128) { GO(128); }
     else if (hd == 64) { GO(64); }
     else { GO(32); }
