@@ -419,14 +419,11 @@ int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows
  * times their sum - from max(0, P - Q) at the failure (P itself if that is zero everywhere), or from P[b][n_draft[b]]; -1 if no weight is
  * positive.  Weights need not sum to one; what is not above zero, a NaN among them, counts as zero.  Sums are in 64 bits.
  * P [rows][gamma + 1][V]: elements (b, j, v) at b * p_row + j * p_pos + v; Q the same; d [rows][gamma], u [rows][gamma], w [rows].
- * Out: n_acc [rows], tokens [rows][gamma + 1]: the accepted drafts, the drawn token, -1 behind it.
- * scratch: METASD_ACCEPT_PROBS_SCRATCH_BYTES, 16-byte aligned, used by one call at a time. */
+ * Out: n_acc [rows], tokens [rows][gamma + 1]: the accepted drafts, the drawn token, -1 behind it. */
 #define METASD_ACCEPT_PROBS_MAX_VOCAB (1 << 20)
-#define METASD_ACCEPT_PROBS_SEGMENT 4096
-#define METASD_ACCEPT_PROBS_SCRATCH_BYTES(rows, V) ((size_t)(rows) * (((size_t)(V) + METASD_ACCEPT_PROBS_SEGMENT - 1) / METASD_ACCEPT_PROBS_SEGMENT) * 16)
 int32_t metasd_accept_probs(const float* P, int64_t p_row, int64_t p_pos, const float* Q, int64_t q_row, int64_t q_pos, const int32_t* d,
                             const int32_t* n_draft, const float* u, const float* w, int32_t rows, int32_t gamma, int32_t V, int32_t* n_acc,
-                            int32_t* tokens, void* scratch, void* hip_stream);
+                            int32_t* tokens, void* hip_stream);
 
 /* ---- measurement aids: not part of the method's boundary (no step of Alg. 1-3 needs them); benchmarks use them to
  * state achieved bandwidth per kernel next to what the machine reaches on a plain read ------------------------- */

@@ -105,7 +105,7 @@ def load_library():
         "metasd_kv_rows": [C.POINTER(_Pages), vp, i32, i32, vp, vp, vp],
         "metasd_attn_pages_scratch": [i32, i32, i32, i32, i32, i32, i32, C.POINTER(sz)],
         "metasd_attn_pages": [C.POINTER(_Pages), i32, i32, i32, vp, i64, vp, i64, vp, i32, i32, vp, vp, i32, i32, f32, vp, sz, vp],
-        "metasd_accept_probs": [vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp],
+        "metasd_accept_probs": [vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -466,32 +466,43 @@ def philox_words(seed: int, c0_start: int, n: int, c1: int, c2: int, c3: int, de
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _on(first: torch.Tensor, *ints: torch.Tensor):
-    """The stream to launch on: the current one of the tensors' device, which has to be the current device.  ints: contiguous int32."""
-    if not first.is_cuda:
+# The current stream's handle by device index: torch.cuda.current_stream() builds an object for it, 2.8 us of a call that takes 8 in all.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _on(first: torch.Tensor, ints) -> int:
+    """The stream to launch on: the current one of the tensors' device, which has to be the current device.  ints: contiguous int32 there."""
+    dev = first.get_device()
+    if dev < 0:
         raise ValueError("tensors on a GPU are needed; there is no CPU fallback")
     for t in ints:
-        if t.dtype != torch.int32 or not t.is_contiguous() or t.device != first.device:
+        if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
             raise ValueError(f"contiguous int32 on {first.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if first.device.index != torch.cuda.current_device():
+    if dev != torch.cuda.current_device():
         raise ValueError(f"the tensors are on {first.device}, which is not the current device")
-    return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(dev)
 
 
 def _rows3(name: str, x: torch.Tensor, rows: int, heads, hd: int, like: torch.Tensor) -> int:
     """Elements between the rows of x: [rows, heads, hd] or [rows, heads * hd], heads next to each other.  heads None: any number of them."""
-    inner = x.stride(-1) == 1 and (x.dim() == 2 or (x.dim() == 3 and x.shape[2] == hd and (x.stride(1) == hd or x.shape[1] == 1)))
-    wide = x.shape[1] * x.shape[2] if x.dim() == 3 else x.shape[1] if x.dim() == 2 else 0
-    if not inner or x.shape[0] != rows or wide == 0 or (wide != heads * hd if heads is not None else wide % hd) or x.dtype != like.dtype or x.device != like.device:
-        raise ValueError(f"{name}: {rows} rows of {'' if heads is None else heads} heads of {hd}, {like.dtype} on {like.device}, heads next to each other; got {tuple(x.shape)} {x.dtype}")
-    return x.stride(0) if rows > 1 else wide
+    shape, stride = x.shape, x.stride()
+    if len(shape) == 2:
+        wide, ok = shape[1], stride[1] == 1
+    elif len(shape) == 3:
+        wide, ok = shape[1] * hd, shape[2] == hd and stride[2] == 1 and (stride[1] == hd or shape[1] == 1)
+    else:
+        wide, ok = 0, False
+    if not ok or shape[0] != rows or wide == 0 or (wide % hd if heads is None else wide != heads * hd) or x.dtype is not like.dtype or x.get_device() != like.get_device():
+        raise ValueError(f"{name}: {rows} rows of {'' if heads is None else heads} heads of {hd}, {like.dtype} on {like.device}, heads next to each other; got {tuple(shape)} {x.dtype}")
+    return stride[0] if rows > 1 else wide
 
 
 def _pages(pool: torch.Tensor, page: int, n_kv_heads: int, head_dim: int) -> _Pages:
     """pool: uint8 [n_pages, bytes of a page], pages any stride apart."""
-    if pool.dtype != torch.uint8 or pool.dim() != 2 or pool.stride(1) != 1 or pool.shape[1] < n_kv_heads * (page // 16) * 17 * head_dim:
-        raise ValueError(f"pool: uint8 [n_pages, page_bytes] with contiguous pages expected, got {pool.dtype} {tuple(pool.shape)}")
-    return _Pages(n_kv_heads, head_dim, page, pool.shape[0], pool.data_ptr(), pool.stride(0) if pool.shape[0] > 1 else pool.shape[1])
+    shape = pool.shape
+    if pool.dtype is not torch.uint8 or len(shape) != 2 or pool.stride(1) != 1 or shape[1] < n_kv_heads * (page // 16) * 17 * head_dim:
+        raise ValueError(f"pool: uint8 [n_pages, page_bytes] with contiguous pages expected, got {pool.dtype} {tuple(shape)}")
+    return _Pages(n_kv_heads, head_dim, page, shape[0], pool.data_ptr(), pool.stride(0) if shape[0] > 1 else shape[1])
 
 
 class Rope:
@@ -513,16 +524,16 @@ def page_plan(table: torch.Tensor, held: torch.Tensor, ring: torch.Tensor, state
               rows: int, out=None) -> dict:
     """metasd_page_plan: table [batch, width], held [batch], ring [n_pages] and state [4] are updated in place.  Returns slots and pos [rows],
     start [batch + 1], served [batch] (out: the same dict, reused)."""
-    _require_gpu()
-    st = _on(table, table, held, ring, state, lens, n_new)
+    st = _on(table, (table, held, ring, state, lens, n_new))
     B, width = table.shape
     if held.numel() != B or lens.numel() != B or n_new.numel() != B or state.numel() < 4:
         raise ValueError("page_plan: held, lens and n_new have one entry per request, state four")
     if out is None:
         buf = torch.empty(2 * rows + 2 * B + 1, dtype=torch.int32, device=table.device)
-        out = dict(slots=buf[:rows], pos=buf[rows:2 * rows], start=buf[2 * rows:2 * rows + B + 1], served=buf[2 * rows + B + 1:])
+        slots, pos, start, served = buf.split((rows, rows, B + 1, B))
+        out = dict(slots=slots, pos=pos, start=start, served=served)
     else:
-        _on(table, out["slots"], out["pos"], out["start"], out["served"])
+        _on(table, (out["slots"], out["pos"], out["start"], out["served"]))
         if out["slots"].numel() < rows or out["pos"].numel() < rows or out["start"].numel() < B + 1 or out["served"].numel() < B:
             raise ValueError("page_plan: out is too small")
     _check(load_library().metasd_page_plan(table.data_ptr(), B, width, held.data_ptr(), ring.data_ptr(), ring.numel(), state.data_ptr(), lens.data_ptr(), n_new.data_ptr(),
@@ -533,10 +544,9 @@ def page_plan(table: torch.Tensor, held: torch.Tensor, ring: torch.Tensor, state
 def rope_append(q, k, v, pos: torch.Tensor, slots, pool, page: int, n_kv_heads: int, head_dim: int, rope: Rope, out=None):
     """metasd_rope_append: q [rows, n_heads (,) head_dim] rotated (returned, [rows, n_heads, head_dim]); k rotated and v appended to the pool at
     `slots`.  q may be None, or k, v, slots and pool."""
-    _require_gpu()
     lead = q if q is not None else k
-    st = _on(lead, pos, *([slots] if k is not None else []))
-    rows, L = lead.shape[0], load_library()
+    st = _on(lead, (pos,) if k is None else (pos, slots))
+    rows = lead.shape[0]
     if pos.numel() != rows or (k is not None and slots.numel() != rows):
         raise ValueError("rope_append: one position and one slot per row")
     H = ldq = ldo = ldk = ldv = 0
@@ -548,25 +558,25 @@ def rope_append(q, k, v, pos: torch.Tensor, slots, pool, page: int, n_kv_heads: 
         ldo = _rows3("out", out, rows, H, head_dim, q)
     if k is not None:
         ldk, ldv = _rows3("k", k, rows, n_kv_heads, head_dim, lead), _rows3("v", v, rows, n_kv_heads, head_dim, lead)
-        if pool.device != lead.device:
+        if pool.get_device() != lead.get_device():
             raise ValueError(f"pool is on {pool.device}")
         pages = _pages(pool, page, n_kv_heads, head_dim)
     else:
         pages = _Pages(n_kv_heads, head_dim, page, 0, None, 0)
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    _check(L.metasd_rope_append(C.byref(rope.c), C.byref(pages), _DTYPES.get(lead.dtype, -1), rows, H, ptr(q), ldq, ptr(out) if q is not None else None, ldo, ptr(k), ldk,
+    _check(load_library().metasd_rope_append(C.byref(rope.c), C.byref(pages), _DTYPES.get(lead.dtype, -1), rows, H, ptr(q), ldq, ptr(out) if q is not None else None, ldo, ptr(k), ldk,
                                 ptr(v), ldv, pos.data_ptr(), ptr(slots) if k is not None else None, st))
     return out
 
 
 def kv_rows(pool: torch.Tensor, slots: torch.Tensor, page: int, n_kv_heads: int, head_dim: int, dtype=torch.float32):
     """metasd_kv_rows: the values held at the slots, k and v [rows, n_kv_heads, head_dim]."""
-    _require_gpu()
-    st = _on(pool, slots)
+    st = _on(pool, (slots,))
     pages = _pages(pool, page, n_kv_heads, head_dim)
-    kv = torch.empty((2, slots.numel(), n_kv_heads, head_dim), dtype=dtype, device=pool.device)
-    _check(load_library().metasd_kv_rows(C.byref(pages), slots.data_ptr(), slots.numel(), _DTYPES.get(dtype, -1), kv[0].data_ptr(), kv[1].data_ptr(), st))
-    return kv[0], kv[1]
+    rows, dev = slots.numel(), pool.device
+    k, v = torch.empty((rows, n_kv_heads, head_dim), dtype=dtype, device=dev), torch.empty((rows, n_kv_heads, head_dim), dtype=dtype, device=dev)
+    _check(load_library().metasd_kv_rows(C.byref(pages), slots.data_ptr(), rows, _DTYPES.get(dtype, -1), k.data_ptr(), v.data_ptr(), st))
+    return k, v
 
 
 @functools.lru_cache(maxsize=256)
@@ -580,45 +590,45 @@ def attn_pages(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, start: 
                max_new: int, max_len: int, out=None) -> torch.Tensor:
     """metasd_attn_pages: q [rows, n_heads, head_dim]; request b's rows are start[b] .. start[b + 1] - 1, its lens[b] positions in the pages
     table[b].  Rows of a new `out` behind the last request are not written."""
-    _require_gpu()
-    st = _on(q, table, start, lens)
+    st = _on(q, (table, start, lens))
     rows, H, hd = q.shape
     B, width = table.shape
-    if start.numel() != B + 1 or lens.numel() != B or pool.device != q.device:
+    if start.numel() != B + 1 or lens.numel() != B or pool.get_device() != q.get_device():
         raise ValueError("attn_pages: start has batch + 1 entries, lens batch, the pool is on the same device")
     if out is None:
         out = torch.empty((rows, H, hd), dtype=q.dtype, device=q.device)
     dt = _DTYPES.get(q.dtype, -1)
     ldq, ldo = _rows3("q", q, rows, H, hd, q), _rows3("out", out, rows, H, hd, q)
     pages = _pages(pool, page, n_kv_heads, hd)
-    n = _attn_scratch(B, H, n_kv_heads, hd, dt, max_new, max_len, q.device.index)
+    n = _attn_scratch(B, H, n_kv_heads, hd, dt, max_new, max_len, q.get_device())
     scratch = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     _check(load_library().metasd_attn_pages(C.byref(pages), dt, rows, H, q.data_ptr(), ldq, out.data_ptr(), ldo, table.data_ptr(), B, width, start.data_ptr(), lens.data_ptr(),
                                             max_new, max_len, scale, scratch.data_ptr() if n else None, n, st))
     return out
 
 
-ACCEPT_PROBS_SEGMENT = 4096
-
-
 def accept_probs(P: torch.Tensor, Q, d: torch.Tensor, n_draft, u: torch.Tensor, w: torch.Tensor, out=None) -> dict:
     """metasd_accept_probs: P [rows, gamma + 1, V] and Q [rows, gamma, V] (or None) fp32 probabilities, d [rows, gamma] int32, n_draft [rows] int32
     (or None), u [rows, gamma] and w [rows] fp32.  Returns n_acc [rows] and tokens [rows, gamma + 1] int32."""
-    _require_gpu()
-    st = _on(P, d, *([n_draft] if n_draft is not None else []))
+    st = _on(P, (d,) if n_draft is None else (d, n_draft))
     rows, g1, V = P.shape
     if d.shape != (rows, g1 - 1) or u.shape != d.shape or w.shape != (rows,) or (n_draft is not None and n_draft.shape != (rows,)) or (Q is not None and Q.shape != (rows, g1 - 1, V)):
         raise ValueError("accept_probs: P [rows, gamma + 1, V], Q [rows, gamma, V], d and u [rows, gamma], w and n_draft [rows]")
     for t in (P, u, w) if Q is None else (P, Q, u, w):
-        if t.dtype != torch.float32 or t.stride(-1) != 1 or t.device != P.device:
+        if t.dtype is not torch.float32 or t.get_device() != P.get_device() or (t.stride(-1) != 1 and t.shape[-1] > 1):
             raise ValueError("accept_probs: fp32 on one device, the last dimension contiguous")
     if not (u.is_contiguous() and w.is_contiguous()):
         raise ValueError("accept_probs: u and w contiguous")
     if out is None:
-        buf = torch.empty(rows * (g1 + 1), dtype=torch.int32, device=P.device)
-        out = dict(n_acc=buf[:rows], tokens=buf[rows:].view(rows, g1))
-    scratch = torch.empty(rows * (-(-V // ACCEPT_PROBS_SEGMENT)) * 16, dtype=torch.uint8, device=P.device)
-    _check(load_library().metasd_accept_probs(P.data_ptr(), P.stride(0), P.stride(1), None if Q is None else Q.data_ptr(), 0 if Q is None else Q.stride(0),
-                                              0 if Q is None else Q.stride(1), d.data_ptr(), None if n_draft is None else n_draft.data_ptr(), u.data_ptr(), w.data_ptr(),
-                                              rows, g1 - 1, V, out["n_acc"].data_ptr(), out["tokens"].data_ptr(), scratch.data_ptr(), st))
+        n_acc, tokens = torch.empty(rows, dtype=torch.int32, device=P.device), torch.empty((rows, g1), dtype=torch.int32, device=P.device)
+        out = dict(n_acc=n_acc, tokens=tokens)
+    else:
+        n_acc, tokens = out["n_acc"], out["tokens"]
+        _on(P, (n_acc, tokens))
+        if n_acc.numel() < rows or tokens.numel() < rows * g1:
+            raise ValueError("accept_probs: out is too small")
+    ps, qs = P.stride(), (0, 0) if Q is None else Q.stride()
+    _check(load_library().metasd_accept_probs(P.data_ptr(), ps[0], ps[1], None if Q is None else Q.data_ptr(), qs[0], qs[1], d.data_ptr(),
+                                              None if n_draft is None else n_draft.data_ptr(), u.data_ptr(), w.data_ptr(), rows, g1 - 1, V, n_acc.data_ptr(),
+                                              tokens.data_ptr(), st))
     return out

@@ -5,139 +5,156 @@
 
 namespace msd {
 
-constexpr int AP_NT = 1024, AP_SEG = 4 * AP_NT;      // threads of a workgroup, tokens of a segment of the vocabulary
+constexpr int AP_NT = 1024, AP_NW = AP_NT / 64, AP_U = 4;      // threads and wavefronts of a workgroup; requests in flight per lane and law
 
 struct AcceptProbs {
     const float *P, *Q;
     size_t p_row, p_pos, q_row, q_pos;      // elements between requests and between positions
     const int *d, *n;
     const float *u, *w;
-    int rows, gamma, V, vec;                // vec: rows of P and Q start on 16 bytes
-    double2* seg;                           // [rows][segments] sums of a segment: (what is drawn from, the target's law)
+    int gamma, V, vec;                      // vec: rows of P and Q start on 16 bytes
     int *n_acc, *tokens;
 };
 
-// The first draft of row b that fails its test u q < p (n: none does).  Every thread gets it.
-__device__ __forceinline__ int first_failure(const AcceptProbs& a, int b, int n, int* sh) {
-    if (threadIdx.x == 0) *sh = n;
+// Four tokens of a law from v on, zeros past the end.
+__device__ __forceinline__ f32x4 law4(const float* p, int v, int V, int vec) {
+    if (vec && v + 3 < V) return *reinterpret_cast<const f32x4*>(p + v);
+    f32x4 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = v + i < V ? p[v + i] : 0.f;
+    return x;
+}
+// What four tokens add to what is drawn from: max(0, p - q) in 64 bits, a NaN nothing; not the token `out`.
+__device__ __forceinline__ void rest4(const f32x4& p, const f32x4& q, int v, int out, double* r) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const bool on = p[e] > q[e] && v + e != out;
+        r[e] = (double)(on ? p[e] : 0.f) - (double)(on ? q[e] : 0.f);
+    }
+}
+// Sum of the weights of the tokens v0 .. v1 - 1 over the wavefront; q == nullptr: zeros.
+__device__ __forceinline__ double span_sum(const float* p, const float* q, int v0, int v1, int V, int vec, int out) {
+    const int lane4 = (threadIdx.x & 63) * 4;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    double sum = 0.0, r[4];
+    int c = v0;
+    if (vec)
+        for (; c + AP_U * 256 <= v1; c += AP_U * 256) {               // requests without a condition: all in flight together
+            f32x4 x[AP_U], y[AP_U];
+#pragma unroll
+            for (int i = 0; i < AP_U; ++i) x[i] = *reinterpret_cast<const f32x4*>(p + c + i * 256 + lane4);
+#pragma unroll
+            for (int i = 0; i < AP_U; ++i) y[i] = q ? *reinterpret_cast<const f32x4*>(q + c + i * 256 + lane4) : zero;
+#pragma unroll
+            for (int i = 0; i < AP_U; ++i) {
+                rest4(x[i], y[i], c + i * 256 + lane4, out, r);
+                sum += (r[0] + r[1]) + (r[2] + r[3]);
+            }
+        }
+    for (; c < v1; c += 256) {
+        const int v = c + lane4;
+        if (v >= v1) break;
+        rest4(law4(p, v, V, vec), q ? law4(q, v, V, vec) : zero, v, out, r);
+        sum += (r[0] + r[1]) + (r[2] + r[3]);
+    }
+    return dpp_sum(sum);
+}
+
+// One workgroup per request.  The tests are exact: u q and p are products and numbers of 24 bits, compared in 64.  Then one row of P - and,
+// behind a rejection, one of Q - is all that is read, once: wavefront i sums the weights of its span of the vocabulary (256 tokens at a time,
+// both in their ascending order), and the one whose span the drawn sum falls into reads that again, from L2, to find the token.
+// What bounds it: for one request the chain n - d - p, q - row - sums - token, for hundreds HBM.   grid (requests), block AP_NT
+__global__ __launch_bounds__(AP_NT, 8) void accept_probs_kernel(AcceptProbs a) {
+    __shared__ int fail, token;
+    __shared__ double rest[AP_NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
+    const int* db = a.d + (size_t)b * a.gamma;
+    const float *pb = a.P + (size_t)b * a.p_row, *qb = a.Q ? a.Q + (size_t)b * a.q_row : nullptr;
+    // ---- the first draft that fails its test
+    const int n = a.n ? min(max(a.n[b], 0), a.gamma) : a.gamma;
+    const float w = a.w[b];
+    if (tid == 0) { fail = n; token = -1; }
     __syncthreads();
-    for (int j = threadIdx.x; j < n; j += AP_NT) {
-        const int t = a.d[(size_t)b * a.gamma + j];
+    for (int j = tid; j < a.gamma; j += AP_NT) {
+        const int t = db[j];
+        const float u = a.u[(size_t)b * a.gamma + j];
+        if (j >= n) continue;
         bool ok = false;
         if (t >= 0 && t < a.V) {
-            const double p = a.P[(size_t)b * a.p_row + (size_t)j * a.p_pos + t], q = a.Q ? (double)a.Q[(size_t)b * a.q_row + (size_t)j * a.q_pos + t] : 1.0;
-            ok = (double)a.u[(size_t)b * a.gamma + j] * q < p;        // exact: two 24-bit factors
+            const float p = pb[(size_t)j * a.p_pos + t], q = qb ? qb[(size_t)j * a.q_pos + t] : 1.f;
+            ok = (double)u * (double)q < (double)p;
         }
-        if (!ok) atomicMin(sh, j);
+        if (!ok) atomicMin(&fail, j);
     }
     __syncthreads();
-    return *sh;
-}
-__device__ __forceinline__ int drafts_of(const AcceptProbs& a, int b) { return a.n ? min(max(a.n[b], 0), a.gamma) : a.gamma; }
-
-// Weights of four tokens from v on: p (what the target gives) and r (what is drawn from: the bonus token from p, else from max(0, p - q)).
-__device__ __forceinline__ void weights4(const AcceptProbs& a, const float* p, const float* q, int out, int v, double* pw, double* rw) {
-    float x[4] = {}, y[4] = {};
-    if (a.vec && v + 3 < a.V) {
-        const float4 f = *reinterpret_cast<const float4*>(p + v);
-        x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
-        if (q) { const float4 h = *reinterpret_cast<const float4*>(q + v); y[0] = h.x; y[1] = h.y; y[2] = h.z; y[3] = h.w; }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (v + i < a.V) { x[i] = p[v + i]; if (q) y[i] = q[v + i]; }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        pw[i] = x[i] > 0.f ? (double)x[i] : 0.0;
-        const double r = (double)x[i] - (double)y[i];
-        rw[i] = v + i == out ? 0.0 : r > 0.0 ? r : 0.0;               // out: the rejected token of a drafter without a law of its own
-    }
-}
-
-// grid (segments, rows), block AP_NT
-__global__ __launch_bounds__(AP_NT) void accept_probs_sum_kernel(AcceptProbs a) {
-    __shared__ int fail;
-    __shared__ double2 red[AP_NT / 64];
-    const int b = blockIdx.y, n = drafts_of(a, b), k = first_failure(a, b, n, &fail);
+    const int k = fail;
     const bool rejected = k < n;
-    const float* p = a.P + (size_t)b * a.p_row + (size_t)k * a.p_pos;
-    const float* q = rejected && a.Q ? a.Q + (size_t)b * a.q_row + (size_t)k * a.q_pos : nullptr;
-    const int out = rejected && !a.Q ? a.d[(size_t)b * a.gamma + k] : -1;
-    double pw[4], rw[4];
-    weights4(a, p, q, out, blockIdx.x * AP_SEG + threadIdx.x * 4, pw, rw);
-    const double ps = dpp_sum((pw[0] + pw[1]) + (pw[2] + pw[3])), rs = dpp_sum((rw[0] + rw[1]) + (rw[2] + rw[3]));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_double2(rs, ps);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double2 t = make_double2(0.0, 0.0);
-        for (int i = 0; i < AP_NT / 64; ++i) { t.x += red[i].x; t.y += red[i].y; }
-        a.seg[(size_t)b * gridDim.x + blockIdx.x] = t;
+    const float* p = pb + (size_t)k * a.p_pos;
+    const float* q = rejected && qb ? qb + (size_t)k * a.q_pos : nullptr;
+    int out = rejected && !qb ? db[k] : -1;            // the rejected draft of a drafter without a law of its own
+    // ---- sums of the wavefronts' spans
+    const int span = (a.V + AP_NW * 256 - 1) / (AP_NW * 256) * 256, v0 = min(wave * span, a.V), v1 = min(v0 + span, a.V);
+    auto total = [&]() {
+        const double s = span_sum(p, q, v0, v1, a.V, a.vec, out);
+        if (lane == 0) rest[wave] = s;
+        __syncthreads();
+        double Z = 0.0;
+        for (int i = 0; i < AP_NW; ++i) Z += rest[i];
+        return Z;
+    };
+    double Z = total();
+    if (rejected && !(Z > 0.0)) {                      // nothing is left of the residual: the target's law itself
+        q = nullptr;
+        out = -1;
+        __syncthreads();
+        Z = total();
     }
-}
-
-// grid (rows), block AP_NT
-__global__ __launch_bounds__(AP_NT) void accept_probs_draw_kernel(AcceptProbs a, int nseg) {
-    __shared__ int fail, token, first[AP_NT / 64], final_[AP_NT / 64];
-    __shared__ double red[AP_NT / 64];
-    const int tid = threadIdx.x, b = blockIdx.x, n = drafts_of(a, b), k = first_failure(a, b, n, &fail);
-    const bool rejected = k < n;
-    const float* p = a.P + (size_t)b * a.p_row + (size_t)k * a.p_pos;
-    const float* q = rejected && a.Q ? a.Q + (size_t)b * a.q_row + (size_t)k * a.q_pos : nullptr;
-    const int out = rejected && !a.Q ? a.d[(size_t)b * a.gamma + k] : -1;
-    double Z = 0.0, Zp = 0.0;
-    for (int i = 0; i < nseg; ++i) { const double2 t = a.seg[(size_t)b * nseg + i]; Z += t.x; Zp += t.y; }
-    const bool from_p = !(Z > 0.0);                    // nothing is left of the residual: the target's law itself
-    const double target = (double)a.w[b] * (from_p ? Zp : Z);
-    double before = 0.0;
-    int s = -1, s_pos = -1;                            // the segment in which the sum passes the target; the last that adds anything
-    double at = 0.0, at_pos = 0.0;
-    for (int i = 0; i < nseg && s < 0; ++i) {
-        const double2 t = a.seg[(size_t)b * nseg + i];
-        const double x = from_p ? t.y : t.x;
-        if (x > 0.0) { s_pos = i; at_pos = before; }
-        if (before + x > target) { s = i; at = before; }
+    // ---- the span that the drawn sum falls into
+    const double target = (double)w * Z;
+    double before = 0.0, base = 0.0;
+    int mine = -1, last = -1;                          // .. or, should rounding leave none, the last with a weight
+    for (int i = 0; i < AP_NW; ++i) {
+        const double x = rest[i];
+        if (x > 0.0) last = i;
+        if (mine < 0 && before + x > target) { mine = i; base = before; }
         before += x;
     }
-    if (s < 0) { s = s_pos; at = at_pos; }
-    if (tid == 0) token = -1;
-    if (s >= 0) {
-        const int v = s * AP_SEG + tid * 4;
-        double pw[4], rw[4];
-        weights4(a, p, q, out, v, pw, rw);
-        double* x = from_p ? pw : rw;
-        const double mine = (x[0] + x[1]) + (x[2] + x[3]), scan = dpp_scan(mine);
-        if ((tid & 63) == 63) red[tid >> 6] = scan;
-        __syncthreads();
-        double base = at;
-        for (int i = 0; i < tid >> 6; ++i) base += red[i];
-        // the first token that passes the target; if rounding leaves none, the last one with a weight
-        const unsigned long long some = __ballot(mine > 0.0), pass = __ballot(mine > 0.0 && base + scan > target);
-        const int lane = tid & 63;
-        if (lane == 0) { first[tid >> 6] = -1; final_[tid >> 6] = -1; }
-        if (pass && lane == __ffsll(pass) - 1) {
-            double run = base + (scan - mine);
-            int pick = -1;
-            bool done = false;
-            for (int i = 0; i < 4; ++i) {
-                run += x[i];
-                if (x[i] > 0.0 && !done) { pick = v + i; done = run > target; }
+    if (mine < 0) mine = last;
+    if (wave == mine) {                                // wavefront-uniform
+        int fallback = -1;
+        bool found = false;
+        for (int c = v0; c < v1 && !found; c += 256) {
+            const int v = c + lane * 4;
+            f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+            if (v < v1) {
+                x = law4(p, v, a.V, a.vec);
+                if (q) y = law4(q, v, a.V, a.vec);
             }
-            first[tid >> 6] = pick;
+            double r[4];
+            rest4(x, y, v, out, r);
+            const double sum = (r[0] + r[1]) + (r[2] + r[3]), scan = dpp_scan(sum);
+            const unsigned long long some = __ballot(sum > 0.0), pass = __ballot(sum > 0.0 && base + scan > target);
+            // the first token at which the sum passes the target, or the last with a weight so far
+            const int at = pass ? __ffsll(pass) - 1 : some ? 63 - __clzll(some) : -1;
+            if (at >= 0) {
+                double run = base + (scan - sum);
+                int pick = -1;
+                bool done = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    run += r[e];
+                    if (r[e] > 0.0 && !done) { pick = v + e; done = pass && run > target; }
+                }
+                fallback = __builtin_amdgcn_readlane(pick, at);
+            }
+            found = pass != 0;
+            base += __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(scan), 63), __builtin_amdgcn_readlane(__double2loint(scan), 63));
         }
-        if (some && lane == 63 - __clzll(some)) final_[tid >> 6] = v + (x[3] > 0.0 ? 3 : x[2] > 0.0 ? 2 : x[1] > 0.0 ? 1 : 0);
-        __syncthreads();
-        if (tid == 0) {
-            int t = -1;
-            for (int i = 0; i < AP_NT / 64 && t < 0; ++i) t = first[i];
-            for (int i = AP_NT / 64 - 1; i >= 0 && t < 0; --i) t = final_[i];
-            token = t;
-        }
+        if (lane == 0) token = fallback;
     }
     __syncthreads();
     if (tid == 0) a.n_acc[b] = k;
-    for (int j = tid; j <= a.gamma; j += AP_NT)
-        a.tokens[(size_t)b * (a.gamma + 1) + j] = j < k ? a.d[(size_t)b * a.gamma + j] : j == k ? token : -1;
+    for (int j = tid; j <= a.gamma; j += AP_NT) a.tokens[(size_t)b * (a.gamma + 1) + j] = j < k ? db[j] : j == k ? token : -1;
 }
 
 }  // namespace msd

@@ -248,20 +248,14 @@ int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows
 }
 
 int32_t metasd_accept_probs(const float* P, int64_t p_row, int64_t p_pos, const float* Q, int64_t q_row, int64_t q_pos, const int32_t* d, const int32_t* n_draft,
-                            const float* u, const float* w, int32_t rows, int32_t gamma, int32_t V, int32_t* n_acc, int32_t* tokens, void* scratch,
-                            void* hip_stream) {
-    if (!P || !d || !u || !w || !n_acc || !tokens || !scratch) return fail_global(METASD_E_INVALID, "accept_probs: NULL pointer (Q and n_draft may be NULL)");
-    if (rows < 1 || rows > 65535 || gamma < 1 || gamma > 1024 || V < 1 || V > METASD_ACCEPT_PROBS_MAX_VOCAB)
-        return fail_global(METASD_E_INVALID, "accept_probs: rows 1..65535, gamma 1..1024, V 1..%d", METASD_ACCEPT_PROBS_MAX_VOCAB);
+                            const float* u, const float* w, int32_t rows, int32_t gamma, int32_t V, int32_t* n_acc, int32_t* tokens, void* hip_stream) {
+    if (!P || !d || !u || !w || !n_acc || !tokens) return fail_global(METASD_E_INVALID, "accept_probs: NULL pointer (Q and n_draft may be NULL)");
+    if (rows < 1 || rows > (1 << 24) || gamma < 1 || gamma > 1024 || V < 1 || V > METASD_ACCEPT_PROBS_MAX_VOCAB)
+        return fail_global(METASD_E_INVALID, "accept_probs: rows 1..2^24, gamma 1..1024, V 1..%d", METASD_ACCEPT_PROBS_MAX_VOCAB);
     if (p_pos < V || (rows > 1 && p_row < V) || (Q && (q_pos < V || (rows > 1 && q_row < V)))) return fail_global(METASD_E_INVALID, "accept_probs: rows of probabilities must not overlap");
-    if (!aligned(scratch)) return fail_global(METASD_E_INVALID, "accept_probs: scratch must be 16-byte aligned");
     const int vec = aligned(P) && p_row % 4 == 0 && p_pos % 4 == 0 && (!Q || (aligned(Q) && q_row % 4 == 0 && q_pos % 4 == 0));
-    const AcceptProbs a{P, Q, (size_t)p_row, (size_t)p_pos, (size_t)q_row, (size_t)q_pos, d, n_draft, u, w, rows, gamma, V, vec, (double2*)scratch, n_acc, tokens};
-    const int nseg = (V + AP_SEG - 1) / AP_SEG;
-    static_assert(METASD_ACCEPT_PROBS_SEGMENT == AP_SEG, "scratch of a row");
-    hipStream_t st = (hipStream_t)hip_stream;
-    hipLaunchKernelGGL(accept_probs_sum_kernel, dim3(nseg, rows), dim3(AP_NT), 0, st, a);
-    hipLaunchKernelGGL(accept_probs_draw_kernel, dim3(rows), dim3(AP_NT), 0, st, a, nseg);
+    const AcceptProbs a{P, Q, (size_t)p_row, (size_t)p_pos, (size_t)q_row, (size_t)q_pos, d, n_draft, u, w, gamma, V, vec, n_acc, tokens};
+    hipLaunchKernelGGL(accept_probs_kernel, dim3(rows), dim3(AP_NT), 0, (hipStream_t)hip_stream, a);
     if (hipGetLastError() != hipSuccess) return fail_global(METASD_E_HIP, "accept_probs: launch failed");
     return METASD_OK;
 }

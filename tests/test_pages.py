@@ -96,13 +96,12 @@ def test_attention_refusals(lib, kw, text):
                                        a["max_new"], a["max_len"], a["scale"], OK, 1 << 30, None), text)
 
 
-@pytest.mark.parametrize("kw,text", [(dict(P=None), "NULL"), (dict(w=None), "NULL"), (dict(scratch=None), "NULL"), (dict(rows=0), "rows"), (dict(rows=65536), "rows"), (dict(gamma=0), "gamma"),
-                                     (dict(gamma=1025), "gamma"), (dict(V=0), "V 1"), (dict(V=(1 << 20) + 1), "V 1"), (dict(p_pos=99), "overlap"), (dict(q_row=5), "overlap"),
-                                     (dict(scratch=OK + 8), "16-byte")])
+@pytest.mark.parametrize("kw,text", [(dict(P=None), "NULL"), (dict(w=None), "NULL"), (dict(rows=0), "rows"), (dict(rows=(1 << 24) + 1), "rows"), (dict(gamma=0), "gamma"),
+                                     (dict(gamma=1025), "gamma"), (dict(V=0), "V 1"), (dict(V=(1 << 20) + 1), "V 1"), (dict(p_pos=99), "overlap"), (dict(q_row=5), "overlap")])
 def test_accept_refusals(lib, kw, text):
-    a = dict(P=OK, p_row=400, p_pos=100, Q=OK, q_row=300, q_pos=100, d=OK, n=OK, u=OK, w=OK, rows=2, gamma=3, V=100, scratch=OK)
+    a = dict(P=OK, p_row=400, p_pos=100, Q=OK, q_row=300, q_pos=100, d=OK, n=OK, u=OK, w=OK, rows=2, gamma=3, V=100)
     a.update(kw)
-    refused(lib, lib.metasd_accept_probs(a["P"], a["p_row"], a["p_pos"], a["Q"], a["q_row"], a["q_pos"], a["d"], a["n"], a["u"], a["w"], a["rows"], a["gamma"], a["V"], OK, OK, a["scratch"], None), text)
+    refused(lib, lib.metasd_accept_probs(a["P"], a["p_row"], a["p_pos"], a["Q"], a["q_row"], a["q_pos"], a["d"], a["n"], a["u"], a["w"], a["rows"], a["gamma"], a["V"], OK, OK, None), text)
 
 
 def test_reference_quantiser():
