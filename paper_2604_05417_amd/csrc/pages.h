@@ -208,6 +208,7 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
 constexpr int ROPE_MAX_PAIRS = 64;
 struct RopeTab {
     int style, rot;          // rot: components that are rotated, 0: none
+    int blocks;              // the rotated components and their partners are whole blocks of eight
     float gain;
     double freq[ROPE_MAX_PAIRS];
 };
@@ -254,35 +255,87 @@ struct RopeArgs {
     T* q_out;
     size_t ldq, ldk, ldv, ldo;
     const int *pos, *slots;
-    int rows, H;
+    int H;
 };
 
-// A workgroup takes RR rows and every gridDim.y-th of their heads; HD / 8 lanes a head, eight components each (a head's lanes are in one
-// wavefront).  Units 0 .. H - 1 are query heads, H .. H + KH - 1 K/V heads.   grid (ceil(rows / RR), splits), block 256
-template <typename T, int HD, int RR>
+// gain * (cos a, sin a) of an angle of up to 2^31 periods, off by some 1e-15 before it is rounded: a less the nearest multiple of pi / 2, taken
+// off in two parts of it, then the Taylor series up to the 14th power (0.79^15 / 15! = 2e-14).
+__device__ __forceinline__ float2 turn_of(double a, double gain) {
+    const double n = rint(a * 0.63661977236758134308);
+    double r = fma(-n, 1.57079632679489661923, a);
+    r = fma(-n, 6.12323399573676588614e-17, r);
+    const double z = r * r;
+    double s = 1.0 / 6227020800.0;
+    s = fma(s, z, -1.0 / 39916800.0);
+    s = fma(s, z, 1.0 / 362880.0);
+    s = fma(s, z, -1.0 / 5040.0);
+    s = fma(s, z, 1.0 / 120.0);
+    s = fma(s, z, -1.0 / 6.0);
+    s = fma(s * z, r, r);
+    double c = -1.0 / 87178291200.0;
+    c = fma(c, z, 1.0 / 479001600.0);
+    c = fma(c, z, -1.0 / 3628800.0);
+    c = fma(c, z, 1.0 / 40320.0);
+    c = fma(c, z, -1.0 / 720.0);
+    c = fma(c, z, 1.0 / 24.0);
+    c = fma(c, z, -0.5);
+    c = fma(c, z, 1.0);
+    const int q = (int)(n - 4.0 * floor(n * 0.25));
+    const double x = q & 1 ? s : c, y = q & 1 ? c : s;
+    return make_float2((float)((q + 1) & 2 ? -x * gain : x * gain), (float)(q & 2 ? -y * gain : y * gain));
+}
+
+// A workgroup takes a row and every gridDim.y-th of its heads, HD / 8 lanes a head, eight components each (a head's lanes are in one
+// wavefront).  Units 0 .. H - 1 are query heads, H .. H + KH - 1 K/V heads.
+// What bounds it: HBM, for few rows the chain position - angle - rows.  1999 rows of 32 + 32 heads of 128 in bf16 (74 MB): 20.3 us, of which 6
+// for the 8.7 MB of codes, whose 16-byte pieces share cache lines with those of the next positions; 16 rows a workgroup, which brings
+// such lines together in one L2, 21.4 us.   grid (rows, splits), block 256
+template <typename T, int HD>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs<T> a, RopeTab rt, Pool pl) {
 #pragma clang fp contract(off)
     constexpr int LN = HD / 8, UN = 256 / LN;         // lanes of a unit, units at a time
-    __shared__ float2 turn[RR][ROPE_MAX_PAIRS];
-    __shared__ float xs[UN][HD + 4];
-    const int tid = threadIdx.x, half = rt.rot >> 1, r0 = blockIdx.x * RR;
-    for (int i = tid; i < RR * half; i += 256) {
-        const int r = i / half, j = i - r * half;
-        if (r0 + r < a.rows) {
-            double sn, cs;
-            sincos((double)a.pos[r0 + r] * rt.freq[j], &sn, &cs);
-            turn[r][j] = make_float2((float)(cs * (double)rt.gain), (float)(sn * (double)rt.gain));
-        }
-    }
+    __shared__ __align__(16) float2 turn[ROPE_MAX_PAIRS];
+    __shared__ __align__(16) float xs[UN][HD + 4];
+    const int tid = threadIdx.x, half = rt.rot >> 1, row = blockIdx.x;
+    if (tid < half) turn[tid] = turn_of((double)a.pos[row] * rt.freq[tid], (double)rt.gain);
     __syncthreads();
     const int u = tid / LN, l = tid % LN, d0 = l * 8;
-    const int HQ = a.q ? a.H : 0, NU = HQ + (a.k ? pl.KH : 0), total = RR * NU;
+    const int HQ = a.q ? a.H : 0, NU = HQ + (a.k ? pl.KH : 0);
     float* x = xs[u];
-    auto rotate = [&](float* y, int r) {               // y: this lane's eight components, in and out
-        __builtin_amdgcn_wave_barrier();
+    // y: this lane's eight components, in and out.  A unit's lanes are in one wavefront, whose LDS accesses are carried out in order.
+    auto rotate = [&](float* y) {
+        if (rt.blocks) {
+            if (d0 >= rt.rot) return;                  // these lanes' partners are at or beyond rt.rot too
+            if (rt.style == 0) {
+                __builtin_amdgcn_wave_barrier();
+                store8(x + d0, y);
+                __builtin_amdgcn_wave_barrier();
+                const bool first = d0 < half;
+                const int j0 = first ? d0 : d0 - half;
+                float o[8], cs[16];
+                load8(x + (first ? d0 + half : j0), o);
+                load8(reinterpret_cast<const float*>(turn + j0), cs);
+                load8(reinterpret_cast<const float*>(turn + j0 + 4), cs + 8);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[d0 + i] = y[i];
-        __builtin_amdgcn_wave_barrier();               // a unit's lanes are in one wavefront, whose LDS accesses are carried out in order
+                for (int i = 0; i < 8; ++i) {
+                    const float p1 = y[i] * cs[2 * i], p2 = o[i] * cs[2 * i + 1];
+                    y[i] = first ? p1 - p2 : p1 + p2;
+                }
+            } else {
+                float cs[8];
+                load8(reinterpret_cast<const float*>(turn + d0 / 2), cs);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a1 = y[2 * i] * cs[2 * i], b1 = y[2 * i + 1] * cs[2 * i + 1], a2 = y[2 * i + 1] * cs[2 * i], b2 = y[2 * i] * cs[2 * i + 1];
+                    y[2 * i] = a1 - b1;
+                    y[2 * i + 1] = a2 + b2;
+                }
+            }
+            return;
+        }
+        __builtin_amdgcn_wave_barrier();
+        store8(x + d0, y);
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int d = d0 + i;
@@ -290,26 +343,25 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs<T> a, RopeTab
             const bool first = rt.style == 0 ? d < half : (d & 1) == 0;
             const int j = rt.style == 0 ? (first ? d : d - half) : d >> 1;
             const float other = x[rt.style == 0 ? (first ? d + half : d - half) : d ^ 1];
-            const float2 cs = turn[r][j];
+            const float2 cs = turn[j];
             const float p1 = y[i] * cs.x, p2 = other * cs.y;
             y[i] = first ? p1 - p2 : p1 + p2;
         }
     };
-    for (int i0 = blockIdx.y * UN; i0 < total; i0 += gridDim.y * UN) {
-        const int i = i0 + u, r = min(i, total - 1) / NU, h = min(i, total - 1) - r * NU, row = r0 + r;
-        const bool on = i < total && row < a.rows;
-        const int rr = min(row, a.rows - 1);
+    for (int i0 = blockIdx.y * UN; i0 < NU; i0 += gridDim.y * UN) {
+        const int h = min(i0 + u, NU - 1);
+        const bool on = i0 + u < NU;
         float y[8];
         if (h < HQ) {
-            load8(a.q + (size_t)rr * a.ldq + (size_t)h * HD + d0, y);
-            rotate(y, r);
-            if (on) store8(a.q_out + (size_t)rr * a.ldo + (size_t)h * HD + d0, y);
+            load8(a.q + (size_t)row * a.ldq + (size_t)h * HD + d0, y);
+            rotate(y);
+            if (on) store8(a.q_out + (size_t)row * a.ldo + (size_t)h * HD + d0, y);
         } else {
-            const int kh = h - HQ, slot = a.slots[rr];
+            const int kh = h - HQ, slot = a.slots[row];
             float z[8];
-            load8(a.k + (size_t)rr * a.ldk + (size_t)kh * HD + d0, y);
-            load8(a.v + (size_t)rr * a.ldv + (size_t)kh * HD + d0, z);
-            rotate(y, r);
+            load8(a.k + (size_t)row * a.ldk + (size_t)kh * HD + d0, y);
+            load8(a.v + (size_t)row * a.ldv + (size_t)kh * HD + d0, z);
+            rotate(y);
             uint32_t ka = 0, va = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {

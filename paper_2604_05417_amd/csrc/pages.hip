@@ -57,6 +57,7 @@ void rope_table(const metasd_rope& r, RopeTab* t) {
     const double n = r.rot_dim, theta = r.theta;
     t->style = r.style;
     t->rot = r.rot_dim;
+    t->blocks = r.rot_dim % (r.style == METASD_ROPE_HALF ? 16 : 8) == 0;
     t->gain = r.gain;
     double a = 0, b = 0;
     if (r.scaling == METASD_ROPE_INDEX) {
@@ -85,26 +86,25 @@ const char* check_rows(const char* what, const T* p, int64_t ld, int64_t n, size
 }
 
 template <typename T, int HD>
-void launch_rope(const RopeArgs<T>& a, const RopeTab& rt, const Pool& pl, int n_cu, hipStream_t st) {
+void launch_rope(const RopeArgs<T>& a, int rows, const RopeTab& rt, const Pool& pl, int n_cu, hipStream_t st) {
     const int units = (a.q ? a.H : 0) + (a.k ? pl.KH : 0);
     constexpr int UN = 256 / (HD / 8);
-    // few rows: one a workgroup, and its heads over several; many rows: 16, whose codes of V share cache lines
-    if (a.rows < 8 * n_cu) {
-        const int splits = std::max(1, std::min((units + UN - 1) / UN, 4 * n_cu / a.rows));
-        hipLaunchKernelGGL((rope_append_kernel<T, HD, 1>), dim3(a.rows, splits), dim3(256), 0, st, a, rt, pl);
-    } else {
-        const int tiles = (a.rows + 15) / 16, splits = std::max(1, std::min((16 * units + UN - 1) / UN, 4 * n_cu / tiles));
-        hipLaunchKernelGGL((rope_append_kernel<T, HD, 16>), dim3(tiles, splits), dim3(256), 0, st, a, rt, pl);
-    }
+    const int splits = std::max(1, std::min((units + UN - 1) / UN, 4 * n_cu / rows));      // few rows: the heads of one over several workgroups
+    hipLaunchKernelGGL((rope_append_kernel<T, HD>), dim3(rows, splits), dim3(256), 0, st, a, rt, pl);
 }
 
 template <int HD, int TERMS>
 void launch_attn(const PagesAttn& a, const Pool& pl, const PagesPlan& p, hipStream_t st) {
-    const dim3 grid((unsigned)((size_t)a.B * pl.KH * a.nsp * a.ncg)), block(64 * PA_NW);
-#define GO(CT, PACK) hipLaunchKernelGGL((attn_pages_kernel<HD, CT, TERMS, PACK>), grid, block, 0, st, a, pl)
-    if (p.ct == 2) GO(2, 1);
-    else if (TERMS == 1 || p.pack == 1) GO(1, 1);
-    else if constexpr (TERMS > 1) { if (p.pack == 2) GO(1, 2); else GO(1, 4); }
+    const dim3 grid((unsigned)((size_t)a.B * pl.KH * a.nsp * a.ncg)), block(64 * p.nw);
+#define GO(CT, PACK, NW) hipLaunchKernelGGL((attn_pages_kernel<HD, CT, TERMS, PACK, NW>), grid, block, 0, st, a, pl)
+#define GO1(PACK) if (p.nw == 16) GO(1, PACK, 16); else GO(1, PACK, 4)
+    if (p.wide) {
+        const dim3 wide((unsigned)(8 * (((size_t)a.B * pl.KH + 7) / 8) * a.nsp * a.ncg));
+        hipLaunchKernelGGL((attn_pages_long_kernel<HD, TERMS>), wide, block, 0, st, a, pl);
+    } else if (p.ct == 2) GO(2, 1, 4);
+    else if (TERMS == 1 || p.pack == 1) { GO1(1); }
+    else if constexpr (TERMS > 1) { if (p.pack == 2) { GO1(2); } else { GO1(4); } }
+#undef GO1
 #undef GO
     if (a.nsp > 1) {
         constexpr int UN = 256 / (HD / 4);
@@ -170,10 +170,10 @@ int32_t metasd_rope_append(const metasd_rope* rope, const metasd_pages* pages, i
     hipStream_t st = (hipStream_t)hip_stream;
 #define GO(T)                                                                                                                                                    \
     {                                                                                                                                                            \
-        const RopeArgs<T> a{(const T*)q, (const T*)k, (const T*)v, (T*)q_out, (size_t)q_ld, (size_t)k_ld, (size_t)v_ld, (size_t)q_out_ld, pos, slots, rows, n_heads}; \
-        if (hd == 128) launch_rope<T, 128>(a, tab, pl, n_cu, st);                                                                                                \
-        else if (hd == 64) launch_rope<T, 64>(a, tab, pl, n_cu, st);                                                                                             \
-        else launch_rope<T, 32>(a, tab, pl, n_cu, st);                                                                                                           \
+        const RopeArgs<T> a{(const T*)q, (const T*)k, (const T*)v, (T*)q_out, (size_t)q_ld, (size_t)k_ld, (size_t)v_ld, (size_t)q_out_ld, pos, slots, n_heads}; \
+        if (hd == 128) launch_rope<T, 128>(a, rows, tab, pl, n_cu, st);                                                                                                \
+        else if (hd == 64) launch_rope<T, 64>(a, rows, tab, pl, n_cu, st);                                                                                             \
+        else launch_rope<T, 32>(a, rows, tab, pl, n_cu, st);                                                                                                           \
     }
     if (dtype == METASD_BF16) GO(bf16_t) else GO(float)
 #undef GO
@@ -207,7 +207,7 @@ int32_t metasd_attn_pages_scratch(int32_t batch, int32_t n_heads, int32_t n_kv_h
     if (dtype != METASD_F32 && dtype != METASD_BF16) return fail_global(METASD_E_INVALID, "attn_pages_scratch: dtype");
     const int n_cu = n_cu_of_device();
     if (!n_cu) return fail_global(METASD_E_HIP, "attn_pages_scratch: cannot query the device");
-    const PagesPlan p = plan_pages(batch, n_kv_heads, n_heads / n_kv_heads, max_new, max_len, dtype == METASD_BF16 ? 1 : 2, n_cu);
+    const PagesPlan p = plan_pages(batch, n_kv_heads, n_heads / n_kv_heads, head_dim, max_new, max_len, dtype == METASD_BF16 ? 1 : 2, n_cu);
     *bytes_out = pages_records(p, batch, n_kv_heads, head_dim) * sizeof(float);
     return METASD_OK;
 }
@@ -230,10 +230,10 @@ int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows
     if (bad) return fail_global(METASD_E_INVALID, "attn_pages: rows of %s must start on 16 bytes and not overlap", bad);
     const int n_cu = n_cu_of_device();
     if (!n_cu) return fail_global(METASD_E_HIP, "attn_pages: cannot query the device");
-    const PagesPlan p = plan_pages(batch, KH, n_heads / KH, max_new, max_len, dtype == METASD_BF16 ? 1 : 2, n_cu);
+    const PagesPlan p = plan_pages(batch, KH, n_heads / KH, hd, max_new, max_len, dtype == METASD_BF16 ? 1 : 2, n_cu);
     const size_t need = pages_records(p, batch, KH, hd) * sizeof(float);
     if (need && (!scratch || !aligned(scratch) || scratch_bytes < need)) return fail_global(METASD_E_WORKSPACE, "attn_pages: scratch of %zu bytes, 16-byte aligned, needed (metasd_attn_pages_scratch)", need);
-    if ((size_t)batch * KH * p.nsp * p.ncg > (size_t)INT32_MAX) return fail_global(METASD_E_INVALID, "attn_pages: too many requests, heads and rows for one launch");
+    if (((size_t)batch * KH + 7) * p.nsp * p.ncg > (size_t)INT32_MAX) return fail_global(METASD_E_INVALID, "attn_pages: too many requests, heads and rows for one launch");
     const PagesAttn a{q, out, (size_t)q_ld, (size_t)out_ld, 0, table, start, lens, (float*)scratch, scale * 1.44269504088896341f, 0, batch, width, rows, n_heads, n_heads / KH,
                       max_new, p.spw, p.nsp, p.ncg};
     const Pool pl = pool_of(*pages);

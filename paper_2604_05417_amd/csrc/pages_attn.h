@@ -87,23 +87,23 @@ __device__ __forceinline__ void pages_store4(const PagesAttn& a, int row, int h,
 // TERMS = 2: q and P as two bf16 terms each.  The maximum is only raised, and O rescaled, when a score exceeds it by more than 2^8; sums are in
 // 32 bits.  The next sub-block is requested while the present one is multiplied.  The wavefronts merge through LDS; a context of one
 // record is written as it is, several are merged by pages_merge_kernel.
-template <int HD, int CT, int TERMS, int PACK>
+template <int HD, int CT, int TERMS, int PACK, int NW>
 struct PagesForm {
     static constexpr int W = 16 / PACK;                               // (row, head) pairs of a column tile
     static constexpr int NQ = PACK == 1 ? TERMS : PACK == 2 ? 2 : 1;  // products per operand of K or V
     static constexpr int Q = CT * (HD / 32) * NQ;                     // operands of q, four registers each
     static constexpr bool QL = Q > 8 || (PACK == 2 && HD == 128);     // more than 32 registers (or what would spill): they stay in LDS
-    static constexpr int OS = HD + 4, LDS = QL && Q * 1024 > PA_NW * 16 * OS * 4 ? Q * 1024 : PA_NW * 16 * OS * 4;
-    static constexpr int WAVES = HD == 128 ? (CT == 1 ? 4 : 2) : HD == 64 ? (CT == 1 ? 4 : 3) : CT == 1 ? 6 : 4;      // per SIMD, without spills
+    static constexpr int OS = HD + 4, LDS = QL && Q * 1024 > NW * 16 * OS * 4 ? Q * 1024 : NW * 16 * OS * 4;
+    static constexpr int WAVES = NW > 4 ? 4 : HD == 128 ? (CT == 1 ? 4 : 2) : HD == 64 ? (CT == 1 ? 4 : 3) : CT == 1 ? 6 : 4;      // per SIMD, without spills
 };
-template <int HD, int CT, int TERMS, int PACK>
-__global__ __launch_bounds__(64 * PA_NW, (PagesForm<HD, CT, TERMS, PACK>::WAVES)) void attn_pages_kernel(PagesAttn a, Pool pl) {
-    typedef PagesForm<HD, CT, TERMS, PACK> F;
+template <int HD, int CT, int TERMS, int PACK, int NW>
+__global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES)) void attn_pages_kernel(PagesAttn a, Pool pl) {
+    typedef PagesForm<HD, CT, TERMS, PACK, NW> F;
     constexpr int KC = HD / 32, OS = F::OS, W = F::W, NQ = F::NQ;
     __shared__ __align__(16) unsigned char lds[F::LDS];
     float* o_sh = reinterpret_cast<float*>(lds);
     u32x4* q_sh = reinterpret_cast<u32x4*>(lds);                      // [column tile][k][term][lane]
-    __shared__ float mx_sh[PA_NW][CT * W], sum_sh[PA_NW][CT * W];
+    __shared__ float mx_sh[NW][CT * W], sum_sh[NW][CT * W];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g = lane >> 4;
     int id = blockIdx.x;
     const int cg = id % a.ncg; id /= a.ncg;
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(64 * PA_NW, (PagesForm<HD, CT, TERMS, PACK>::WAVES)
         const size_t at = (size_t)(rq.row0 + r) * a.ldq + (size_t)h * HD + g * 8;
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
-            if (F::QL && ((ct * KC + k) & (PA_NW - 1)) != wave) continue;          // each wavefront brings a part
+            if (F::QL && ((ct * KC + k) & (NW - 1)) != wave) continue;          // each wavefront brings a part
             u32x4 x[NQ];
             if constexpr (TERMS == 1) x[0] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const bf16_t*>(a.q) + at + k * 32);
             else {
@@ -165,15 +165,15 @@ __global__ __launch_bounds__(64 * PA_NW, (PagesForm<HD, CT, TERMS, PACK>::WAVES)
     uint32_t ks[2];
     const int tshift = pl.shift - 4, tlast = max(seen - 1, 0) >> 4;
     const int* tab = a.table + (size_t)b * a.width;
-    const int first = sp * a.spw + wave;               // this wavefront's sub-blocks: first, first + PA_NW, ..
+    const int first = sp * a.spw + wave;               // this wavefront's sub-blocks: first, first + NW, ..
     // page numbers of the next 32 sub-blocks, two tiles each, one a lane: a request finds them in a register
     int ids = 0;
     auto look_up = [&](int k) {
-        const int tile = min(2 * (first + (k + (lane >> 1)) * PA_NW) + (lane & 1), tlast);       // past the end: the last tile again, whose weights are zero there
+        const int tile = min(2 * (first + (k + (lane >> 1)) * NW) + (lane & 1), tlast);       // past the end: the last tile again, whose weights are zero there
         ids = (int)min((unsigned)tab[tile >> tshift], (unsigned)(pl.n_pages - 1));
     };
     auto place = [&](int k, int t) {
-        const int tile = min(2 * (first + k * PA_NW) + t, tlast);
+        const int tile = min(2 * (first + k * NW) + t, tlast);
         return tile_at<HD>(pl, __builtin_amdgcn_readlane(ids, (k & 31) * 2 + t), kh, tile & ((1 << tshift) - 1));
     };
     const unsigned char *at0, *at1;                    // the tiles of the sub-block whose V is still to be requested
@@ -202,9 +202,9 @@ __global__ __launch_bounds__(64 * PA_NW, (PagesForm<HD, CT, TERMS, PACK>::WAVES)
         request_k(0);
         request_v();
     }
-    for (int s = first, k = 0; s < s1; s += PA_NW, ++k) {
+    for (int s = first, k = 0; s < s1; s += NW, ++k) {
         const int p0 = s * 32;
-        const bool more = s + PA_NW < s1;
+        const bool more = s + NW < s1;
         if (more && ((k + 1) & 31) == 0) look_up(k + 1);
         // ---- scores
         __builtin_amdgcn_s_setprio(1);
@@ -361,16 +361,16 @@ __global__ __launch_bounds__(64 * PA_NW, (PagesForm<HD, CT, TERMS, PACK>::WAVES)
             *reinterpret_cast<f32x4*>(dst + 4) = f32x4{o[ct][j][0][2], o[ct][j][1][2], o[ct][j][0][3], o[ct][j][1][3]};
         }
         __syncthreads();
-        for (int i = tid; i < W * (HD / 4); i += 64 * PA_NW) {
+        for (int i = tid; i < W * (HD / 4); i += 64 * NW) {
             const int k = i / (HD / 4), d = (i - k * (HD / 4)) * 4, cc = ct * W + k, c = c0 + cc;
             if (c >= ncol) break;                      // columns ascend
             float M = mx_sh[0][cc];
 #pragma unroll
-            for (int w = 1; w < PA_NW; ++w) M = fmaxf(M, mx_sh[w][cc]);
+            for (int w = 1; w < NW; ++w) M = fmaxf(M, mx_sh[w][cc]);
             f32x4 y = {0.f, 0.f, 0.f, 0.f};
             float tot = 0.f;
 #pragma unroll
-            for (int w = 0; w < PA_NW; ++w) {
+            for (int w = 0; w < NW; ++w) {
                 const float f = mx_sh[w][cc] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx_sh[w][cc] - M);
                 f32x4 x = *reinterpret_cast<const f32x4*>(o_sh + (w * 16 + k) * OS + d);
 #pragma unroll
@@ -387,6 +387,192 @@ __global__ __launch_bounds__(64 * PA_NW, (PagesForm<HD, CT, TERMS, PACK>::WAVES)
             }
         }
     }
+}
+
+// The same for long blocks (prompts): every one of the four wavefronts has 16 columns of its own and all walk the same positions, 64 at a time.
+// Each widens one tile of 16 positions into LDS as the operands that all of them multiply with, so that a position is widened once for 64
+// columns; while they multiply, the codes of the next 64 are on their way.  One buffer, so that four workgroups share a CU: with two
+// buffers and half as many 56 instead of 44 us (1500 rows, 32 heads of 128, bf16), with 32 columns a wavefront 55, with a second team of four for
+// every other step 46; the kernel above, which widens for 32 columns, 51.  What bounds it: nearly as many cycles in LDS (32 KiB read per
+// wavefront and step, 1024) as in the exponentials and the widening (800) and in the products (512).
+// LDS layout: [K: tile][chunk][lane] and [V: pair of tiles][chunk][even, odd][lane], 16 bytes a lane.
+// Workgroup ids deal the (request, K/V head) pairs out over the 8 XCDs, so that the column groups of one share an L2, longest first.
+template <int HD, int TERMS>
+__global__ __launch_bounds__(256, TERMS == 1 ? 4 : 3) void attn_pages_long_kernel(PagesAttn a, Pool pl) {
+    constexpr int KC = HD / 32, OS = HD + 4, GC = 64;  // columns of the workgroup
+    __shared__ u32x4 k_sh[4][KC][64];
+    __shared__ u32x4 v_sh[2][KC][2][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+    const int y = blockIdx.x >> 3, per = a.ncg * a.nsp, unit = (blockIdx.x & 7) + 8 * (y / per), rest = y % per;
+    if (unit >= a.B * pl.KH) return;                   // workgroup-uniform, as are the next two
+    const int cg = a.ncg - 1 - rest / a.nsp, sp = rest % a.nsp, b = unit / pl.KH, kh = unit - b * pl.KH;
+    const PagesReq rq = pages_req(a, b, pl.shift);
+    const int ncol = rq.n * a.G;
+    if (cg * GC >= ncol) return;
+    const int seen = pages_seen(rq, a.G, cg * GC, GC), nsub = (seen + 31) / 32, nrec = pages_records_of(a, seen);
+    if (sp >= nrec) return;
+    const int it0 = sp * a.spw / 2, it1 = ((sp == nrec - 1 ? nsub : min(nsub, (sp + 1) * a.spw)) + 1) / 2;      // steps of 64 positions
+    const int c0 = cg * GC + wave * 16;
+    const int mine = c0 < ncol ? pages_seen(rq, a.G, c0, 16) : 0, all_see = rq.L - rq.n + c0 / a.G;       // positions that some (every) column of the wavefront sees
+    const int c = c0 + col, rc = min(c, ncol - 1) / a.G, h = kh * a.G + (min(c, ncol - 1) - rc * a.G);
+    const int lim = c < ncol ? min(rq.L - rq.n + rc, rq.L - 1) : -1;
+    u32x4 qf[KC][TERMS];
+#pragma unroll
+    for (int k = 0; k < KC; ++k) {
+        const size_t at = (size_t)(rq.row0 + rc) * a.ldq + (size_t)h * HD + g * 8 + k * 32;
+        if constexpr (TERMS == 1) qf[k][0] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const bf16_t*>(a.q) + at);
+        else {
+            float f[8];
+            load8(reinterpret_cast<const float*>(a.q) + at, f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t t[TERMS];
+                terms_of<TERMS>(f[2 * i], f[2 * i + 1], t);
+#pragma unroll
+                for (int u = 0; u < TERMS; ++u) qf[k][u][i] = t[u];
+            }
+        }
+    }
+    f32x4 o[KC][2];
+    float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < KC; ++j) o[j][0] = o[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int tshift = pl.shift - 4, tlast = max(seen - 1, 0) >> 4;
+    const int* tab = a.table + (size_t)b * a.width;
+    Words<KC> kd, vd, vs;
+    uint32_t ks;
+    int ids = 0;
+    auto look_up = [&](int it) {                       // page numbers of this wavefront's tiles in its next 64 steps, one a lane
+        const int tile = min(4 * (it + lane) + wave, tlast);
+        ids = (int)min((unsigned)tab[tile >> tshift], (unsigned)(pl.n_pages - 1));
+    };
+    auto request = [&](int it) {                       // past the end: the last tile again, whose weights are zero there
+        const int tile = min(4 * it + wave, tlast);
+        const unsigned char* p = tile_at<HD>(pl, __builtin_amdgcn_readlane(ids, (it - it0) & 63), kh, tile & ((1 << tshift) - 1));
+        kd = load_words<KC>(p + lane * Tile<HD>::LB);
+        vd = load_words<KC>(p + Tile<HD>::V + lane * Tile<HD>::LB);
+        if constexpr (HD == 128) ks = *reinterpret_cast<const uint32_t*>(p + Tile<HD>::KS + col * 4);
+        else if constexpr (HD == 64) ks = *reinterpret_cast<const uint16_t*>(p + Tile<HD>::KS + col * 2);
+        else ks = p[Tile<HD>::KS + col];
+        vs = load_words<KC>(p + Tile<HD>::VS + g * Tile<HD>::LB);
+    };
+    auto stage = [&](int it) {
+        // positions past the end: whatever lies there, V's scale must not make it infinite
+        const int ok = min(max(rq.L - ((4 * it + wave) * 16 + 4 * g), 0), 4);
+        const uint32_t keep = ok == 4 ? 0xffffffffu : (1u << (8 * ok)) - 1;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+            const float f = c == 0 ? scale_of<0>(ks) : c == 1 ? scale_of<1>(ks) : c == 2 ? scale_of<2>(ks) : scale_of<3>(ks);
+            k_sh[wave][c][lane] = u32x4{PAGES_CVT(kd.w[c], f, 0), PAGES_CVT(kd.w[c], f, 1), PAGES_CVT(kd.w[c], f, 2), PAGES_CVT(kd.w[c], f, 3)};
+        }
+#pragma unroll
+        for (int j = 0; j < KC; ++j) {
+            const uint32_t w = vd.w[j], f = vs.w[j] & keep;
+            const uint32_t x0 = PAGES_CVT(w, scale_of<0>(f), 0), x1 = PAGES_CVT(w, scale_of<1>(f), 1), x2 = PAGES_CVT(w, scale_of<2>(f), 2), x3 = PAGES_CVT(w, scale_of<3>(f), 3);
+            uint2* even = reinterpret_cast<uint2*>(&v_sh[wave >> 1][j][0][lane]) + (wave & 1);
+            uint2* odd = reinterpret_cast<uint2*>(&v_sh[wave >> 1][j][1][lane]) + (wave & 1);
+            *even = make_uint2(__builtin_amdgcn_perm(x1, x0, 0x05040100u), __builtin_amdgcn_perm(x3, x2, 0x05040100u));
+            *odd = make_uint2(__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u));
+        }
+    };
+    if (it0 < it1) {
+        look_up(it0);
+        request(it0);
+    }
+    for (int it = it0; it < it1; ++it) {
+        const int p0 = it * 64;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");            // the readers of the step before are done
+        stage(it);
+        if (it + 1 < it1) {
+            if (((it + 1 - it0) & 63) == 0) look_up(it + 1);
+            request(it + 1);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");            // this step is staged
+        if (p0 >= mine) continue;                      // wavefront-uniform: none of its columns sees these
+        __builtin_amdgcn_s_setprio(1);
+        f32x4 sc[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KC; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const bf16x8 kf = __builtin_bit_cast(bf16x8, k_sh[t][k][lane]);
+#pragma unroll
+                for (int u = TERMS - 1; u >= 0; --u) sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, qf[k][u]), sc[t], 0, 0, 0);
+            }
+        __builtin_amdgcn_s_setprio(0);
+        if (p0 + 63 > all_see) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) sc[t][v] = p0 + t * 16 + g * 4 + v <= lim ? sc[t][v] : -INFINITY;
+        }
+        float m = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) m = fmaxf(m, fmaxf(fmaxf(sc[t][0], sc[t][1]), fmaxf(sc[t][2], sc[t][3])));
+        m = column_max(m) * a.scale2;
+        if (__any(m > mx + 8.f)) {
+            const float nm = fmaxf(mx, m), alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx - nm);
+            mx = nm;
+            sum *= alpha;
+#pragma unroll
+            for (int j = 0; j < KC; ++j) { o[j][0] *= alpha; o[j][1] *= alpha; }
+        }
+        u32x4 pf[2][TERMS];
+        const float base = mx == -INFINITY ? 0.f : mx;
+        float part = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][v], a.scale2, -base));
+                sc[t][v] = e;
+                part += e;
+            }
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                uint32_t w[TERMS];
+                terms_of<TERMS>(sc[t][2 * v], sc[t][2 * v + 1], w);
+#pragma unroll
+                for (int u = 0; u < TERMS; ++u) pf[t >> 1][u][2 * (t & 1) + v] = w[u];
+            }
+        }
+        sum += part;
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < KC; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const bf16x8 vf = __builtin_bit_cast(bf16x8, v_sh[s][j][e][lane]);
+#pragma unroll
+                    for (int u = TERMS - 1; u >= 0; --u) o[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pf[s][u]), o[j][e], 0, 0, 0);
+                }
+        __builtin_amdgcn_s_setprio(0);
+    }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (c >= ncol) return;
+    // every lane has eight neighbouring dimensions of its column per chunk: 32 j + 8 g .. + 7
+    const int cc = wave * 16 + col;
+    float* rec = nrec == 1 ? nullptr : a.rec + (((((size_t)b * pl.KH + kh) * a.ncg + cg) * a.nsp + sp) * GC + cc) * OS;
+    const float inv = rec ? 1.f : sum == 0.f ? 0.f : 1.0f / sum;          // a row that sees nothing: zeros
+#pragma unroll
+    for (int j = 0; j < KC; ++j) {
+        const f32x4 x = o[j][0] * inv, y = o[j][1] * inv;
+        const f32x4 lo = f32x4{x[0], y[0], x[1], y[1]}, hi = f32x4{x[2], y[2], x[3], y[3]};
+        const int d = 32 * j + 8 * g;
+        if (rec) {
+            *reinterpret_cast<f32x4*>(rec + d) = lo;
+            *reinterpret_cast<f32x4*>(rec + d + 4) = hi;
+        } else {
+            pages_store4<TERMS>(a, rq.row0 + rc, h, HD, d, lo);
+            pages_store4<TERMS>(a, rq.row0 + rc, h, HD, d + 4, hi);
+        }
+    }
+    if (rec && g == 0) *reinterpret_cast<float2*>(rec + HD) = make_float2(mx, sum);
 }
 
 // Records of a column merged in their order.  HD / 4 lanes per (request, row, head).   grid ceil(B max_new H / units), block 256

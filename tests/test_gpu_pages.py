@@ -284,6 +284,17 @@ def test_attention_of_long_contexts(dt, H, KH, hd, L, n):
         check_attn(q, pool, table, K, V, [L], [n], 64, KH, 1 / math.sqrt(hd), max_new=n + 5, max_len=hint)
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,KH,hd,page", [(2, 2, 32, 16), (4, 2, 64, 64), (2, 1, 128, 32), (1, 1, 64, 128)])
+def test_attention_of_prompts(dt, H, KH, hd, page):
+    """Long blocks among short and empty ones: prompts, the rest of a prompt behind its prefix, rows that see nothing."""
+    rng = np.random.default_rng(hd + page)
+    lens, n_new = [0, 300, 350, 17, 600, 1, 250], [0, 300, 260, 17, 30, 1, 270]
+    pool, table, K, V = filled(rng, lens, KH, hd, page)
+    q = torch.randn((sum(n_new), H, hd), generator=torch.Generator().manual_seed(6)).to(dt).to(DEV)
+    check_attn(q, pool, table, K, V, lens, n_new, page, KH, 1 / math.sqrt(hd))
+
+
 def test_attention_with_large_scores_and_marked_positions():
     """Scores of hundreds (the weight is on one position); a marked position makes the rows that see it NaN and no others."""
     rng = np.random.default_rng(8)
