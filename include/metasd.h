@@ -149,7 +149,7 @@ int32_t metasd_pack_weight(void* dst, const void* src, int32_t n_out, int32_t n_
 
 /* Create a context.  Descriptors and pointer tables are copied; the device memory they point
  * to stays owned by the caller and must outlive the context.  target_kv / drafter_kv[k] are
- * KV caches of batch * metasd_kv_bytes() each; workspace is >= metasd_workspace_bytes() and 256-byte
+ * KV caches of batch * metasd_kv_bytes() each (target_kv NULL: metasd_set_target_pages follows); workspace is >= metasd_workspace_bytes() and 256-byte
  * aligned.  Errors: INVALID (NULL, unsupported shape: see metasd_last_error), WORKSPACE, HIP. */
 int32_t metasd_create(metasd_ctx** out, const metasd_config* cfg, const metasd_model_desc* target,
                       const metasd_model_desc* drafters /*[K]*/, const void* const* target_weights,
@@ -284,6 +284,24 @@ int32_t metasd_verify_tree(metasd_ctx*);
  * the round is N_acc / (depth of the tree): pass that depth as `gamma` to metasd_bandit_update.
  * Synchronises.  Errors: ORDER, HIP. */
 int32_t metasd_accept_tree(metasd_ctx*, int32_t* n_acc_out, int32_t* token_out, int32_t* path_out);
+
+/* ---- the target's cache in 4-bit pages ------------------------------------------------------------------------------
+ * A context whose (bf16) target keeps its K and V in the 4-bit pages described below instead of target_kv, which may then be NULL at
+ * metasd_create: 17/64 of the bytes per position, in pages that sequences take as they grow and give back when a query ends or drafts are
+ * rejected, so that the pool need not hold batch * max_ctx positions.  K is kept with its rotary pairs next to each other (dimension 2 i of a
+ * head is i, 2 i + 1 is i + head_dim / 2).  Prefill and verification take metasd_page_plan, metasd_rope_append and the attention of
+ * metasd_attn_pages; the target's logits are those of a cache rounded to 4 bits, the rounds' law is Alg. 3's for that target.
+ * Not with token trees, drafter heads, drafters that share the target's cache, or fp32 targets.
+ * kv_prefilled contexts: metasd_set_context takes the pages of the n - 1 positions (they are listed in the table); the caller then writes
+ * them, layer by layer, before the next metasd_draft.
+ *
+ * Bytes of a page (all layers) and of the book, whose first ints are the block table [batch][ceil(max_ctx / page)]. */
+int32_t metasd_target_pages_bytes(const metasd_config* cfg, const metasd_model_desc* target, int32_t page, int32_t n_pages,
+                                  size_t* page_bytes_out, size_t* book_bytes_out);
+/* pool: n_pages pages; book: device memory; both the caller's, 16-byte aligned.  After metasd_create and before the first
+ * metasd_set_context.  A query that finds too few pages is refused by metasd_set_context or metasd_draft (OVERFLOW).
+ * Errors: INVALID, ORDER, WORKSPACE, HIP. */
+int32_t metasd_set_target_pages(metasd_ctx*, void* pool, int32_t n_pages, int32_t page, void* book, size_t book_bytes);
 
 /* ---- stand-alone kernels on caller-supplied logits (device) ------------------------------------ */
 

@@ -16,7 +16,8 @@ EXPORTS = ["metasd_kv_bytes", "metasd_workspace_bytes", "metasd_pack_weight", "m
            "metasd_set_context", "metasd_swap_weight", "metasd_bandit_select", "metasd_bandit_update",
            "metasd_bandit_state", "metasd_draft", "metasd_verify", "metasd_accept", "metasd_draft_tree", "metasd_verify_tree", "metasd_accept_tree", "metasd_accept_logits",
            "metasd_accept_logits_noalloc", "metasd_sample_logits", "metasd_philox_words", "metasd_stream_read", "metasd_profile", "metasd_profile_read", "metasd_profile_shapes", "metasd_peek", "metasd_state", "metasd_state_seq", "metasd_accept_fallbacks", "metasd_set_drafter_head", "metasd_last_error",
-           "metasd_page_bytes", "metasd_page_plan", "metasd_rope_append", "metasd_kv_rows", "metasd_attn_pages_scratch", "metasd_attn_pages", "metasd_accept_probs"]
+           "metasd_page_bytes", "metasd_page_plan", "metasd_rope_append", "metasd_kv_rows", "metasd_attn_pages_scratch", "metasd_attn_pages", "metasd_accept_probs",
+           "metasd_target_pages_bytes", "metasd_set_target_pages"]
 
 
 class MetaSDError(RuntimeError):
@@ -99,6 +100,8 @@ def load_library():
         "metasd_state": [vp, i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)],
         "metasd_state_seq": [vp, i32, i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)],
         "metasd_accept_fallbacks": [vp, C.POINTER(C.c_int64)],
+        "metasd_target_pages_bytes": [C.POINTER(_Config), C.POINTER(_Desc), i32, i32, C.POINTER(sz), C.POINTER(sz)],
+        "metasd_set_target_pages": [vp, vp, i32, i32, vp, sz],
         "metasd_page_bytes": [i32, i32, i32, C.POINTER(sz)],
         "metasd_page_plan": [vp, i32, i32, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp],
         "metasd_rope_append": [C.POINTER(_RopeSpec), C.POINTER(_Pages), i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp],
@@ -157,8 +160,10 @@ class MetaSD:
     def __init__(self, target, drafters, gamma_max: int, max_ctx: int, temperature: float, seed: int,
                  ucb_beta: float = 1.0, reward: str = "BE", device: str = "cuda:0", policy: str = "ucb",
                  policy_param: float = 0.0, policy_window: int = 0, batch: int = 1, share_target_kv: bool = False,
-                 stream=None, heads=None):
-        """stream = (sinks, window): drafters with caches of their own keep a streaming cache (metasd_config.stream_*).
+                 stream=None, heads=None, target_pages=None):
+        """target_pages = (n_pages, page): the target's cache lies in 4-bit pages (metasd_set_target_pages): `page_pool` [n_pages, bytes of a
+        page], `page_table` [batch, pages of max_ctx] int32.
+        stream = (sinks, window): drafters with caches of their own keep a streaming cache (metasd_config.stream_*).
         heads = {k: W_fc [d, 2 d]}: drafter k is a head on the target's hidden states (metasd_set_drafter_head)."""
         _require_gpu()
         self.L = load_library()
@@ -167,6 +172,8 @@ class MetaSD:
         self.gamma_max = gamma_max
         self.max_ctx = max_ctx
         self.batch = batch
+        if target_pages and share_target_kv:
+            raise ValueError("drafters that share the target's cache read it in bf16, not in 4-bit pages")
         self._packed = {}       # data_ptr of a row-major matrix -> packed tensor (early-exit drafters share the target's)
         self._keep = []
         tdesc, tw = target
@@ -179,7 +186,7 @@ class MetaSD:
         self._ddesc_c = (_Desc * self.K)(*[_desc(d) for d in self.ddescs])
         self._tw = self._table(tdesc, tw)
         self._dw = [self._table(d, w) for d, w in drafters]
-        self.kv_target = self._alloc_kv(self._tdesc_c, tdesc)
+        self.kv_target = None if target_pages else self._alloc_kv(self._tdesc_c, tdesc)
         # share_target_kv: a drafter whose layer tensors ARE the target's first layers (early exit) gets the target's cache
         # itself (metasd.h, "shared" strategy); every other drafter gets a cache of its own
         self.kv_shared = [share_target_kv and d["n_layers"] <= tdesc["n_layers"] and
@@ -196,9 +203,19 @@ class MetaSD:
         h = C.c_void_p()
         torch.cuda.synchronize(self.device)
         _check(self.L.metasd_create(C.byref(h), C.byref(self.cfg), C.byref(self._tdesc_c), self._ddesc_c, tptr, dtab,
-                                    self.kv_target.data_ptr(), dkv, self.workspace.data_ptr(), nbytes.value,
+                                    None if target_pages else self.kv_target.data_ptr(), dkv, self.workspace.data_ptr(), nbytes.value,
                                     _stream_ptr(self.stream)))
         self._h = h
+        if target_pages:
+            n_pages, page = (int(v) for v in target_pages)
+            pb, bb = C.c_size_t(0), C.c_size_t(0)
+            _check(self.L.metasd_target_pages_bytes(C.byref(self.cfg), C.byref(self._tdesc_c), page, n_pages, C.byref(pb), C.byref(bb)))
+            self.page_pool = torch.empty((n_pages, pb.value), dtype=torch.uint8, device=self.device)
+            self._book = torch.zeros(bb.value // 4, dtype=torch.int32, device=self.device)
+            width = -(-max_ctx // page)
+            self.page_table = self._book[:batch * width].view(batch, width)
+            torch.cuda.synchronize(self.device)
+            _check(self.L.metasd_set_target_pages(self._h, self.page_pool.data_ptr(), n_pages, page, self._book.data_ptr(), bb.value), self._h)
         for k, fc in (heads or {}).items():
             want = torch.bfloat16 if tdesc["dtype"] == 1 else torch.float32
             assert fc.dtype == want and tuple(fc.shape) == (tdesc["d_model"], 2 * tdesc["d_model"])

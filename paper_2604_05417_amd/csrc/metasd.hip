@@ -61,6 +61,19 @@ constexpr size_t FULLK_LDS_MAX = 150 * 1024;   // gemm_fullk_residual_kernel: th
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 size_t elem_size(const metasd_model_desc& d) { return d.dtype == METASD_BF16 ? 2 : 4; }
 
+// The target's cache in 4-bit pages (metasd_set_target_pages).  A page holds a stretch of positions in every layer, layer_bytes apart.
+struct PagedKV {
+    metasd_pages pages{};           // pool: layer 0
+    size_t layer_bytes = 0;
+    int width = 0;                  // pages that max_ctx positions take
+    int *table = nullptr, *held = nullptr, *ring = nullptr, *state = nullptr, *lens = nullptr, *n_new = nullptr, *total = nullptr, *slots = nullptr, *pos = nullptr,
+        *start = nullptr, *served = nullptr;        // the caller's book
+    std::vector<int> host_held;     // what `held` will be once the launches so far have run
+    bool on() const { return table != nullptr; }
+    int pages_of(int positions) const { return (positions + pages.page - 1) / pages.page; }
+    metasd_pages layer(int L) const { metasd_pages p = pages; p.pool = (char*)p.pool + (size_t)L * layer_bytes; return p; }
+};
+
 struct Model {
     metasd_model_desc d{};
     std::vector<const void*> w;
@@ -74,6 +87,7 @@ struct Model {
     bool stream = false;    // a drafter with a streaming cache (cfg.stream_sink, cfg.stream_window): see forward()
     int tail = 0;           // streaming cache: first position of the contiguous tail (what lies between the sinks and it was skipped)
     const void** d_table = nullptr;   // device copy of w
+    PagedKV paged;
     const void* layer_w(int L, int i) const { return w[1 + PER_LAYER * L + i]; }
     const void* final_norm() const { return w[1 + PER_LAYER * d.n_layers]; }
     const void* lm_head() const { return w[2 + PER_LAYER * d.n_layers]; }
@@ -230,8 +244,31 @@ struct GridBar { int abort; int pad[3]; };
 // Workspace layout shared by metasd_workspace_bytes and metasd_create.
 constexpr size_t INV_BYTES = 128;       // 1/rms of 16 rows; places of 16 rows in a plane of the cache
 struct Layout {
-    size_t hist, h, h2, xn, part, gx, ssq, inv, q, ao, act, apart, rope, P, Q, cand, bd, res, draft, tstep, feat, fest, bar, xchg, chain, tables, table_stride, total;
+    size_t hist, h, h2, xn, part, gx, ssq, inv, q, ao, act, apart, apart_floats, rope, P, Q, cand, bd, res, draft, tstep, feat, fest, bar, xchg, chain, tables, table_stride, total;
 };
+
+// The caller's book of a paged target, in ints: the block table first.
+struct Book { size_t table, held, ring, state, lens, n_new, total, slots, pos, start, served, ints; int width; };
+int paged_rows(const metasd_config& c, const metasd_model_desc& t) { return std::max(MAX_ROWS * c.batch, big_ok(t) ? big_rows(c) : 0); }
+Book make_book(const metasd_config& c, const metasd_model_desc& t, int page, int n_pages) {
+    Book b{};
+    size_t o = 0;
+    auto take = [&](size_t n) { const size_t at = o; o += (n + 3) / 4 * 4; return at; };
+    b.width = (c.max_ctx + page - 1) / page;
+    b.table = take((size_t)c.batch * b.width);
+    b.held = take(c.batch);
+    b.ring = take(n_pages);
+    b.state = take(4);
+    b.lens = take(c.batch);
+    b.n_new = take(c.batch);
+    b.total = take(c.batch);
+    b.slots = take(paged_rows(c, t));
+    b.pos = take(paged_rows(c, t));
+    b.start = take(c.batch + 1);
+    b.served = take(c.batch);
+    b.ints = o;
+    return b;
+}
 
 Layout make_layout(const metasd_config& c, const metasd_model_desc& t, const metasd_model_desc* dr) {
     int dmax = t.d_model, fmax = t.d_ffn, vmax = t.vocab, hmax = t.n_heads, hdmax = t.d_model / t.n_heads;
@@ -287,7 +324,8 @@ Layout make_layout(const metasd_config& c, const metasd_model_desc& t, const met
     L.q = take(RM * dmax * 4);
     L.ao = take(RM * dmax * 4);
     L.act = take(RM * std::max(fmax, c.feature_heads ? 2 * dmax : 0) * 4);   // a drafter head's input rows, 2 d wide, are staged here too
-    L.apart = take(B * hmax * nchunks * 16 * (hdmax + 2) * 4);
+    L.apart_floats = B * hmax * nchunks * 16 * (hdmax + 2);
+    L.apart = take(L.apart_floats * 4);
     L.rope = take(RM * (hdmax / 2) * sizeof(double2));
     L.P = take(B * (c.gamma_max + 1) * vmax * 4);
     L.Q = take(B * c.gamma_max * vmax * 4);
@@ -1283,10 +1321,28 @@ int forward(metasd_ctx* c, Model& M, int pos0, int n, float* logits, bool want_a
     return rc;
 }
 
+int forward_segs(metasd_ctx* c, Model& M, const Segs& sg, float* logits, int out_seq_rows, int out_row0, int last_only);
+
 int forward_blocks(metasd_ctx* c, Model& M, int pos0, int n, float* logits, bool want_all) {
     c->cur_model = model_index(c, M);
     if (pos0 + n > c->cfg.max_ctx) return c->fail(METASD_E_OVERFLOW, "positions %d..%d exceed max_ctx %d", pos0, pos0 + n, c->cfg.max_ctx);
     int done = 0;
+    if (M.paged.on()) {
+        // the paths of a batch serve its one sequence too: a long block, then blocks of at most 16 rows, the last of which may carry logits
+        const int rows = n - (logits ? (want_all ? n : 1) : 0);
+        if (big_ok(M.d) && rows > MAX_ROWS) {
+            if (int rc = forward_big(c, M, 0, pos0, rows)) return rc;
+            done = rows;
+        }
+        while (done < n) {
+            Segs sg{};
+            sg.n = 1; sg.ms = sg.m[0] = std::min(MAX_ROWS, n - done); sg.pos0[0] = pos0 + done;
+            const bool last = done + sg.ms == n;
+            if (int rc = forward_segs(c, M, sg, last ? logits : nullptr, want_all ? sg.ms : 1, 0, want_all ? 0 : 1)) return rc;
+            done += sg.ms;
+        }
+        return 0;
+    }
     // long blocks: everything but the row that carries logits goes through in big blocks
     const int rows = n - (logits ? 1 : 0);
     if (big_ok(M.d) && !c->tree && rows > MAX_ROWS && big_pays(M.d, pos0, rows, 1)) {
@@ -1572,6 +1628,74 @@ void launch_addnorm_many(metasd_ctx* c, int R, float* h, const float* part, int 
         hipLaunchKernelGGL(addnorm_kernel<T>, dim3(R), dim3(1024), 0, c->stream, h, part, ns, (size_t)R * D, D, gain, eps, xn, split);
 }
 
+// ---- a target whose cache lies in 4-bit pages: what a block needs before its layers, and of each layer what the cache takes part in
+
+// Pages, slots and positions for the block sg (segments in the order of their sequences, all of one length).  What a sequence holds beyond
+// the block goes back; pages that go back can be taken from the next plan on, so where only they are left the plan runs twice.
+int plan_paged(metasd_ctx* c, Model& M, const Segs& sg) {
+    PagedKV& pk = M.paged;
+    const int B = c->cfg.batch;
+    PageLens l{};
+    for (int b = 0; b < B; ++b) l.lens[b] = c->sq[b].ready ? M.kvl[b] : 0;
+    for (int s = 0; s < sg.n; ++s) {
+        if (sg.m[s] != sg.ms || (s && sg.seq[s] <= sg.seq[s - 1])) return c->fail(METASD_E_INVALID, "paged target: a block of unequal segments");
+        l.lens[sg.seq[s]] = sg.pos0[s];
+        l.n_new[sg.seq[s]] = sg.ms;
+    }
+    auto plan = [&](bool give_back) -> int {
+        PageLens p = l;
+        int rows = 0;
+        for (int b = 0; b < B; ++b) {
+            if (give_back) p.n_new[b] = 0;
+            rows += p.n_new[b];
+            pk.host_held[b] = pk.pages_of(p.lens[b] + p.n_new[b]);
+        }
+        HIP_TRY(c, page_lens_set(p, B, pk.lens, pk.n_new, pk.total, c->stream));
+        if (metasd_page_plan(pk.table, B, pk.width, pk.held, pk.ring, pk.pages.n_pages, pk.state, pk.lens, pk.n_new, pk.pages.page, std::max(1, rows), pk.slots, pk.pos, pk.start,
+                             pk.served, c->stream))
+            return c->fail(METASD_E_HIP, "page plan: %s", g_err.c_str());
+        return 0;
+    };
+    int held = 0, take = 0, need = 0;
+    for (int b = 0; b < B; ++b) {
+        const int n = pk.pages_of(l.lens[b] + l.n_new[b]);
+        held += pk.host_held[b];
+        need += n;
+        take += std::max(0, n - pk.host_held[b]);
+    }
+    if (need > pk.pages.n_pages) return c->fail(METASD_E_OVERFLOW, "paged target: %d pages needed, %d there", need, pk.pages.n_pages);
+    if (take > pk.pages.n_pages - held)
+        if (int rc = plan(true)) return rc;
+    return plan(false);
+}
+
+// q of the block in d_q (rotated, fp32), K and V in their pages, from the ns sets of q | k | v sums in d_part.  The q and k projections are
+// packed with the members of a rotary pair next to each other (metasd_pack_weight); q and K keep that order, scores do not notice.
+int paged_append(metasd_ctx* c, const Model& M, int L, int R, int ns) {
+    const metasd_model_desc& d = M.d;
+    const int DQ = d.n_heads * M.hd, DKV = d.n_kv_heads * M.hd, N = DQ + 2 * DKV;
+    float* x = c->d_part();
+    HIP_TRY(c, sum_sets(x, ns, (size_t)R * N, c->stream));
+    const metasd_rope rope{METASD_ROPE_PAIRS, M.hd, METASD_ROPE_PLAIN, 0, d.rope_theta, 1.f, 0.f, 0.f, 1.f};
+    const metasd_pages pages = M.paged.layer(L);
+    if (metasd_rope_append(&rope, &pages, METASD_F32, R, d.n_heads, x, N, c->d_q(), DQ, x + DQ, N, x + DQ + DKV, N, M.paged.pos, M.paged.slots, c->stream))
+        return c->fail(METASD_E_HIP, "paged target: %s", g_err.c_str());
+    return 0;
+}
+
+// The rows' attention into d_ao.
+int paged_attention(metasd_ctx* c, const Model& M, int L, int R, int max_new, int max_len) {
+    const metasd_model_desc& d = M.d;
+    const PagedKV& pk = M.paged;
+    const size_t DQ = (size_t)d.n_heads * M.hd;
+    const AttnPagesCall a{(const float*)c->d_q(), c->d_ao(), DQ, DQ, (size_t)R * DQ, rows_split(R), R, d.n_heads, pk.table, pk.start, pk.total, c->cfg.batch, pk.width,
+                          max_new, max_len, 1.0f / sqrtf((float)M.hd), c->d_apart(), c->lay.apart_floats};
+    const bool timed = c->prof_begin(METASD_PROF_ATTN, 2.0 * d.n_kv_heads * M.hd * 17 / 32 * max_len * (R / max_new) + 2.0 * R * DQ * 4);
+    HIP_TRY(c, attn_pages_f32(pk.layer(L), a, c->n_cu, c->stream));
+    if (timed) c->prof_end();
+    return 0;
+}
+
 // Forward of the block sg through model M; appends K/V of the valid rows.  logits == nullptr: none.
 // Otherwise the rows that carry logits are written to logits[(seq * out_seq_rows + out_row0 + j) * V]
 // (last_only: only the last valid row of each segment, at j = 0).
@@ -1594,12 +1718,17 @@ int forward_segs_t(metasd_ctx* c, Model& M, const Segs& sg, float* logits, int o
     hipLaunchKernelGGL(rope_table_seg_kernel, dim3(R), dim3(hd / 2), 0, st, sg, hd, d.rope_theta, c->d_rope(), (long long*)nullptr, (size_t)0);
     LAUNCH_CHECK(c, "rope_table (segments)");
     const SegAttn at = plan_segs(c, d, hd, sg);
+    int max_len = 1;
+    for (int s = 0; s < sg.n; ++s) max_len = std::max(max_len, sg.pos0[s] + sg.m[s]);
+    if (M.paged.on())
+        if ((rc = plan_paged(c, M, sg))) return rc;
     for (int L = 0; L < d.n_layers; ++L) {
         launch_addnorm_many<T>(c, R, h, part, ns, D, (const T*)M.layer_w(L, 0), d.rms_eps, xn, split);
         LAUNCH_CHECK(c, "addnorm");
         if ((rc = gemm_rows<T>(c, xn, D, R, D, M.layer_w(L, 1), DQ, M.layer_w(L, 2), DKV, M.layer_w(L, 3), DKV, &ns))) return rc;
         T* kc = (T*)M.kv + (size_t)L * 2 * plane;
-        if (sizeof(T) == 2 && R >= ROPE4_ROWS && hd >= 64)
+        if (M.paged.on()) { if ((rc = paged_append(c, M, L, R, ns))) return rc; }
+        else if (sizeof(T) == 2 && R >= ROPE4_ROWS && hd >= 64)
             hipLaunchKernelGGL(rope_kv4_seg_kernel, dim3((NQKV + 1023) / 1024, R), dim3(256), 0, st, part, ns, (size_t)R * NQKV, NQKV, sg, H, KH, hd,
                                (const double2*)c->d_rope(), (bf16_t*)c->d_q(), (bf16_t*)kc, (bf16_t*)(kc + plane), seq_stride, c->cfg.max_ctx);
         else
@@ -1607,7 +1736,7 @@ int forward_segs_t(metasd_ctx* c, Model& M, const Segs& sg, float* logits, int o
                                (const double2*)c->d_rope(), (float*)c->d_q(), kc, kc + plane, seq_stride, c->cfg.max_ctx, sizeof(T) == 2 ? 1 : 0,
                                (split && hd >= 64) ? 1 : 0);
         LAUNCH_CHECK(c, "rope_kv (segments)");
-        if ((rc = attention_seg<T>(c, M, L, sg, at))) return rc;
+        if ((rc = M.paged.on() ? paged_attention(c, M, L, R, sg.ms, max_len) : attention_seg<T>(c, M, L, sg, at))) return rc;
         if ((rc = gemm_rows_add<T>(c, c->d_ao(), R, DQ, M.layer_w(L, 4), D, h, &ns))) return rc;
         launch_addnorm_many<T>(c, R, h, part, ns, D, (const T*)M.layer_w(L, 5), d.rms_eps, xn, split);
         LAUNCH_CHECK(c, "addnorm");
@@ -1702,6 +1831,11 @@ int forward_big(metasd_ctx* c, Model& M, int seq, int pos0, int n) {
         hipLaunchKernelGGL(embed_rope_kernel<T>, dim3(m), dim3(320), 0, st, c->d_hist() + (size_t)seq * c->cfg.max_ctx + p0, (const T*)M.w[0], D,
                            h, p0, hd, d.rope_theta, c->d_rope(), TreeBlk{});
         LAUNCH_CHECK(c, "embed + rope table");
+        if (M.paged.on()) {
+            Segs sg{};
+            sg.n = 1; sg.ms = m; sg.seq[0] = seq; sg.m[0] = m; sg.pos0[0] = p0;
+            if ((rc = plan_paged(c, M, sg))) return rc;
+        }
         if (M.head) {   // W_fc . [embedding ; the target's feature of the position before]
             float* cat = (float*)c->d_act();
             hipLaunchKernelGGL(feat_cat_kernel, dim3(m), dim3(256), 0, st, (const float*)h, (const float*)c->d_feat(), (const float*)nullptr,
@@ -1718,8 +1852,11 @@ int forward_big(metasd_ctx* c, Model& M, int seq, int pos0, int n) {
             launch_addnorm_many<T>(c, m, h, part, ns, D, (const T*)M.layer_w(L, 0), d.rms_eps, xn, split);
             LAUNCH_CHECK(c, "addnorm");
             T* kc = kv + (size_t)L * 2 * plane;
-            const RowsPlan* pl = m > MAX_ROWS ? &rows_plan(c, NQKV / 16, D / 32, m, 1, BEHIND_ROPE) : nullptr;
-            if (pl && pl->ksplit == 1) {
+            const RowsPlan* pl = m > MAX_ROWS && !M.paged.on() ? &rows_plan(c, NQKV / 16, D / 32, m, 1, BEHIND_ROPE) : nullptr;
+            if (M.paged.on()) {
+                if ((rc = gemm_rows<T>(c, xn, D, m, D, M.layer_w(L, 1), DQ, M.layer_w(L, 2), DKV, M.layer_w(L, 3), DKV, &ns))) return rc;
+                if ((rc = paged_append(c, M, L, m, ns))) return rc;
+            } else if (pl && pl->ksplit == 1) {
                 metasd_ctx::ProfRec* pr = c->prof_take(METASD_PROF_GEMM, (double)NQKV * D * 2 + (double)m * D * 4 + (double)m * NQKV * 4, NQKV, D, m);
                 const TilesEpi ep{0, 0, (const double2*)c->d_rope(), kc, kc + plane, H, KH, hd, p0, c->cfg.max_ctx};
                 if ((rc = launch_gemm_tiles_any<TILES_ROPE>(c, TilesLaunch{(const bf16_t*)xn, m, D, M.layer_w(L, 1), M.layer_w(L, 2), M.layer_w(L, 3), DQ / 16,
@@ -1735,7 +1872,7 @@ int forward_big(metasd_ctx* c, Model& M, int seq, int pos0, int n) {
                 LAUNCH_CHECK(c, "rope_kv");
             }
             if (L + 1 == d.n_layers && !features) break;
-            if ((rc = attention_big(c, d, hd, kc, kc + plane, p0, m))) return rc;
+            if ((rc = M.paged.on() ? paged_attention(c, M, L, m, m, p0 + m) : attention_big(c, d, hd, kc, kc + plane, p0, m))) return rc;
             if ((rc = gemm_rows_add<T>(c, c->d_ao(), m, DQ, M.layer_w(L, 4), D, h, &ns))) return rc;
             launch_addnorm_many<T>(c, m, h, part, ns, D, (const T*)M.layer_w(L, 5), d.rms_eps, xn, split);
             LAUNCH_CHECK(c, "addnorm");
@@ -1760,7 +1897,7 @@ int forward_segs(metasd_ctx* c, Model& M, const Segs& sg, float* logits, int out
     for (int s = 0; s < sg.n; ++s)
         if (sg.pos0[s] + sg.m[s] > c->cfg.max_ctx)
             return c->fail(METASD_E_OVERFLOW, "sequence %d: positions %d..%d exceed max_ctx %d", sg.seq[s], sg.pos0[s], sg.pos0[s] + sg.m[s], c->cfg.max_ctx);
-    if (segs_step_ok(c, M, sg.n * sg.ms)) return forward_segs_step(c, M, sg, logits, out_seq_rows, out_row0, last_only);
+    if (!M.paged.on() && segs_step_ok(c, M, sg.n * sg.ms)) return forward_segs_step(c, M, sg, logits, out_seq_rows, out_row0, last_only);
     if (M.d.dtype == METASD_BF16) return forward_segs_t<bf16_t>(c, M, sg, logits, out_seq_rows, out_row0, last_only);
     return forward_segs_t<float>(c, M, sg, logits, out_seq_rows, out_row0, last_only);
 }
@@ -2233,7 +2370,7 @@ int32_t metasd_create(metasd_ctx** out, const metasd_config* cfg, const metasd_m
     if (!out) return fail_global(METASD_E_INVALID, "NULL out");
     *out = nullptr;
     if (int rc = check_config(cfg, target, drafters)) return rc;
-    if (!target_weights || !drafter_weights || !target_kv || !drafter_kv || !workspace) return fail_global(METASD_E_INVALID, "NULL pointer argument");
+    if (!target_weights || !drafter_weights || !drafter_kv || !workspace) return fail_global(METASD_E_INVALID, "NULL pointer argument");
     if ((uintptr_t)workspace % ALIGN) return fail_global(METASD_E_INVALID, "workspace must be 256-byte aligned");
     const Layout lay = make_layout(*cfg, *target, drafters);
     if (workspace_bytes < lay.total) return fail_global(METASD_E_WORKSPACE, "workspace too small: need %zu bytes, got %zu", lay.total, workspace_bytes);
@@ -2250,7 +2387,7 @@ int32_t metasd_create(metasd_ctx** out, const metasd_config* cfg, const metasd_m
             if (!M.w[i] && !(gate && d.act == METASD_GELU)) return fail_global(METASD_E_INVALID, "%s: weight %d is NULL", who, i);
             if ((uintptr_t)M.w[i] % 16) return fail_global(METASD_E_INVALID, "%s: weight %d is not 16-byte aligned", who, i);
         }
-        if (!kv || (uintptr_t)kv % 16) return fail_global(METASD_E_INVALID, "%s: KV cache NULL or misaligned", who);
+        if ((!kv && w != target_weights) || (uintptr_t)kv % 16) return fail_global(METASD_E_INVALID, "%s: KV cache NULL or misaligned", who);
         return 0;
     };
     metasd_ctx* c = new (std::nothrow) metasd_ctx();
@@ -2267,7 +2404,7 @@ int32_t metasd_create(metasd_ctx** out, const metasd_config* cfg, const metasd_m
             char who[32];
             snprintf(who, sizeof who, "drafter %d", k);
             rc = fill(c->drafters[k], drafters[k], drafter_weights[k], drafter_kv[k], who);
-            if (!rc && drafter_kv[k] == target_kv) {
+            if (!rc && target_kv && drafter_kv[k] == target_kv) {
                 // shared cache: the drafter must be the target's first layers, tensor for tensor, or its K/V would not be the target's
                 Model& D = c->drafters[k];
                 const metasd_model_desc &a = D.d, &b = *target;
@@ -2362,6 +2499,13 @@ int32_t metasd_set_context(metasd_ctx* c, int32_t seq, const int32_t* tokens, in
         if (tokens[i] < 0 || tokens[i] >= c->target.d.vocab) return c->fail(METASD_E_INVALID, "set_context: token %d out of range at %d", tokens[i], i);
     if (c->phase == PH_DRAFTED || c->phase == PH_VERIFIED || c->phase == PH_TREE_DRAFTED || c->phase == PH_TREE_VERIFIED)
         return c->fail(METASD_E_ORDER, "set_context: a round is in flight (finish it with metasd_accept first)");
+    if (!c->target.kv && !c->target.paged.on()) return c->fail(METASD_E_ORDER, "set_context: the context was created without a cache for the target: call metasd_set_target_pages first");
+    if (c->target.paged.on()) {
+        int need = c->target.paged.pages_of(n + c->cfg.gamma_max);         // of a round of the sequences that are there
+        for (int b = 0; b < c->cfg.batch; ++b)
+            if (b != seq && c->sq[b].ready) need += c->target.paged.pages_of(c->sq[b].l + c->cfg.gamma_max);
+        if (need > c->target.paged.pages.n_pages) return c->fail(METASD_E_OVERFLOW, "set_context: %d pages needed for the target's cache, %d there", need, c->target.paged.pages.n_pages);
+    }
     HIP_TRY(c, hipStreamSynchronize(c->stream));
     metasd_ctx::SeqState& S = c->sq[seq];
     std::copy(tokens, tokens + n, S.hist.begin());
@@ -2376,6 +2520,8 @@ int32_t metasd_set_context(metasd_ctx* c, int32_t seq, const int32_t* tokens, in
     c->phase = all ? PH_READY : PH_NONE;
     c->target.kvl[seq] = kv_prefilled ? n - 1 : 0;
     for (auto& d : c->drafters) { d.kvl[seq] = (kv_prefilled || d.shared_kv) ? n - 1 : 0; d.tail = 0; }
+    if (kv_prefilled && c->target.paged.on())        // pages for what the caller is about to write, listed in the book's table
+        if (int rc = plan_paged(c, c->target, Segs{})) return rc;
     if (!kv_prefilled && n > 1) {
         if (c->cfg.batch == 1) { if (int rc = forward(c, c->target, 0, n - 1, nullptr, false)) return rc; }
         else if (big_ok(c->target.d) && n - 1 > MAX_ROWS) { if (int rc = forward_big(c, c->target, seq, 0, n - 1)) return rc; }
@@ -2444,11 +2590,56 @@ int32_t metasd_set_drafter_head(metasd_ctx* c, int32_t k, const void* w_fc) {
     return METASD_OK;
 }
 
+int32_t metasd_target_pages_bytes(const metasd_config* cfg, const metasd_model_desc* target, int32_t page, int32_t n_pages, size_t* page_bytes_out, size_t* book_bytes_out) {
+    if (!cfg || !target || !page_bytes_out || !book_bytes_out) return fail_global(METASD_E_INVALID, "target_pages_bytes: NULL pointer");
+    char buf[256];
+    if (const char* e = check_model(*target, "target", buf, sizeof buf)) return fail_global(METASD_E_INVALID, "target_pages_bytes: %s", e);
+    if (target->dtype != METASD_BF16) return fail_global(METASD_E_INVALID, "target_pages_bytes: bf16 models only");
+    if (cfg->batch < 1 || cfg->batch > METASD_MAX_BATCH || cfg->max_ctx < 1) return fail_global(METASD_E_INVALID, "target_pages_bytes: batch or max_ctx out of range");
+    size_t layer = 0;
+    if (int rc = metasd_page_bytes(target->n_kv_heads, target->d_model / target->n_heads, page, &layer)) return rc;
+    if (n_pages < 1 || (int64_t)n_pages * page > INT32_MAX) return fail_global(METASD_E_INVALID, "target_pages_bytes: n_pages * page must be within 31 bits");
+    *page_bytes_out = layer * target->n_layers;
+    *book_bytes_out = make_book(*cfg, *target, page, n_pages).ints * sizeof(int32_t);
+    return METASD_OK;
+}
+
+int32_t metasd_set_target_pages(metasd_ctx* c, void* pool, int32_t n_pages, int32_t page, void* book, size_t book_bytes) {
+    if (!c) return fail_global(METASD_E_INVALID, "NULL ctx");
+    size_t page_bytes = 0, need = 0;
+    if (metasd_target_pages_bytes(&c->cfg, &c->target.d, page, n_pages, &page_bytes, &need)) return c->fail(METASD_E_INVALID, "%s", g_err.c_str());
+    if (!pool || (uintptr_t)pool % 16 || !book || (uintptr_t)book % 16) return c->fail(METASD_E_INVALID, "set_target_pages: pool and book must be 16-byte aligned");
+    if (book_bytes < need) return c->fail(METASD_E_WORKSPACE, "set_target_pages: book too small: need %zu bytes, got %zu", need, book_bytes);
+    if (c->cfg.feature_heads) return c->fail(METASD_E_INVALID, "set_target_pages: not with drafter heads on the target's hidden states");
+    for (const auto& D : c->drafters)
+        if (D.shared_kv) return c->fail(METASD_E_INVALID, "set_target_pages: drafters that share the target's cache read it in bf16");
+    for (const auto& q : c->sq)
+        if (q.ready) return c->fail(METASD_E_ORDER, "set_target_pages: call it before the first metasd_set_context");
+    PagedKV& pk = c->target.paged;
+    const Book b = make_book(c->cfg, c->target.d, page, n_pages);
+    int* x = (int*)book;
+    pk.pages = metasd_pages{c->target.d.n_kv_heads, c->target.hd, page, n_pages, pool, page_bytes};
+    pk.layer_bytes = page_bytes / c->target.d.n_layers;
+    pk.width = b.width;
+    pk.table = x + b.table; pk.held = x + b.held; pk.ring = x + b.ring; pk.state = x + b.state;
+    pk.lens = x + b.lens; pk.n_new = x + b.n_new; pk.total = x + b.total;
+    pk.slots = x + b.slots; pk.pos = x + b.pos; pk.start = x + b.start; pk.served = x + b.served;
+    pk.host_held.assign(c->cfg.batch, 0);
+    HIP_TRY(c, page_book_init(pk.table, c->cfg.batch, pk.width, pk.held, pk.ring, n_pages, pk.state, c->stream));
+    return METASD_OK;
+}
+
 int32_t metasd_draft(metasd_ctx* c, const int32_t* k, int32_t gamma) {
     if (!c) return fail_global(METASD_E_INVALID, "NULL ctx");
     if (!k || k[0] < 0 || k[0] >= c->cfg.K) return c->fail(METASD_E_INVALID, "draft: drafter index out of range");
     if (gamma < 1 || gamma > c->cfg.gamma_max) return c->fail(METASD_E_INVALID, "draft: gamma %d not in 1..%d", gamma, c->cfg.gamma_max);
     if (c->phase != PH_READY) return c->fail(METASD_E_ORDER, "draft: call set_context first (for every sequence) / finish the previous round with accept");
+    if (c->target.paged.on()) {
+        const PagedKV& pk = c->target.paged;
+        int need = 0;
+        for (const auto& q : c->sq) need += pk.pages_of(q.l + gamma);
+        if (need > pk.pages.n_pages) return c->fail(METASD_E_OVERFLOW, "draft: %d pages needed to verify %d drafts, %d there", need, gamma, pk.pages.n_pages);
+    }
     if (c->cfg.batch > 1) {
         if (int rc = draft_batch(c, k, gamma)) return rc;
         c->cur_gamma = gamma;
@@ -2575,6 +2766,7 @@ int32_t metasd_draft_tree(metasd_ctx* c, int32_t k, const metasd_tree* tree) {
     if (!c) return fail_global(METASD_E_INVALID, "NULL ctx");
     if (c->cfg.batch != 1) return c->fail(METASD_E_INVALID, "draft_tree: contexts with one sequence only");
     if (k < 0 || k >= c->cfg.K || !tree) return c->fail(METASD_E_INVALID, "draft_tree: bad drafter index or NULL tree");
+    if (c->target.paged.on()) return c->fail(METASD_E_INVALID, "draft_tree: a target whose cache lies in 4-bit pages verifies chains only");
     if (c->drafters[k].stream) return c->fail(METASD_E_INVALID, "draft_tree: drafters with a streaming cache draft chains only");
     if (c->phase != PH_READY) return c->fail(METASD_E_ORDER, "draft_tree: call set_context first / finish the previous round");
     const int n = tree->n;

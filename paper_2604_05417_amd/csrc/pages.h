@@ -2,6 +2,7 @@
 #pragma once
 
 #include "common.h"
+#include "pages_host.h"
 
 namespace msd {
 
@@ -199,6 +200,27 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
         a.state[1] = min(count - taken + all_r, a.n_pages);
         a.state[2] = 0;
     }
+}
+
+// grid 1, block 1024
+__global__ void page_book_init_kernel(int* __restrict__ table, int entries, int* __restrict__ held, int batch, int* __restrict__ ring, int n_pages, int* __restrict__ state) {
+    for (int i = threadIdx.x; i < entries; i += blockDim.x) table[i] = 0;
+    for (int i = threadIdx.x; i < batch; i += blockDim.x) held[i] = 0;
+    for (int i = threadIdx.x; i < n_pages; i += blockDim.x) ring[i] = i;
+    if (threadIdx.x < 4) state[threadIdx.x] = threadIdx.x == 1 ? n_pages : 0;
+}
+// grid 1, block 64
+__global__ void page_lens_kernel(PageLens l, int batch, int* __restrict__ lens, int* __restrict__ n_new, int* __restrict__ total) {
+    const int b = threadIdx.x;
+    if (b < batch) { lens[b] = l.lens[b]; n_new[b] = l.n_new[b]; total[b] = l.lens[b] + l.n_new[b]; }
+}
+// grid ceil(n4 / 256), block 256
+__global__ void sum_sets_kernel(f32x4* x, int ns, size_t n4) {
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n4) return;
+    f32x4 y = x[i];
+    for (int s = 1; s < ns; ++s) y += x[(size_t)s * n4 + i];
+    x[i] = y;
 }
 
 // ------------------------------------------------------------------------------------------

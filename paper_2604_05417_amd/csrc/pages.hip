@@ -113,6 +113,16 @@ void launch_attn(const PagesAttn& a, const Pool& pl, const PagesPlan& p, hipStre
     }
 }
 
+// dtype as in metasd_attn_pages
+void launch_attn_any(const metasd_pages& pages, int dtype, const PagesAttn& a, const PagesPlan& p, hipStream_t st) {
+    const Pool pl = pool_of(pages);
+#define GO(HD) if (dtype == METASD_BF16) launch_attn<HD, 1>(a, pl, p, st); else launch_attn<HD, 3>(a, pl, p, st)
+    if (pages.head_dim == 128) { GO(128); }
+    else if (pages.head_dim == 64) { GO(64); }
+    else { GO(32); }
+#undef GO
+}
+
 // nullptr, or what is wrong with the sizes of an attention call
 const char* check_attn(int32_t batch, int32_t n_heads, int32_t KH, int32_t hd, int32_t max_new, int32_t max_len) {
     if (batch < 1 || batch > 65535) return "batch must be 1..65535";
@@ -122,6 +132,37 @@ const char* check_attn(int32_t batch, int32_t n_heads, int32_t KH, int32_t hd, i
 }
 
 }  // namespace
+
+namespace msd {
+
+hipError_t attn_pages_f32(const metasd_pages& pages, const AttnPagesCall& c, int n_cu, hipStream_t st) {
+    const int KH = pages.n_kv_heads;
+    const PagesPlan p = plan_pages(c.batch, KH, c.H / KH, pages.head_dim, c.max_new, c.max_len, 3, n_cu, c.rec_floats);
+    if (pages_records(p, c.batch, KH, pages.head_dim) > c.rec_floats) return hipErrorOutOfMemory;      // (one span needs none)
+    const PagesAttn a{c.q, c.out, c.ldq, c.ldo, c.lo_off, c.table, c.start, c.lens, c.rec, c.scale * 1.44269504088896341f, c.split, c.batch, c.width, c.rows, c.H, c.H / KH,
+                      c.max_new, p.spw, p.nsp, p.ncg};
+    launch_attn_any(pages, METASD_F32, a, p, st);
+    return hipGetLastError();
+}
+
+hipError_t page_book_init(int* table, int batch, int width, int* held, int* ring, int n_pages, int* state, hipStream_t st) {
+    hipLaunchKernelGGL(page_book_init_kernel, dim3(1), dim3(1024), 0, st, table, batch * width, held, batch, ring, n_pages, state);
+    return hipGetLastError();
+}
+
+hipError_t page_lens_set(const PageLens& l, int batch, int* lens, int* n_new, int* total, hipStream_t st) {
+    static_assert(METASD_MAX_BATCH <= 64, "one lane per request");
+    hipLaunchKernelGGL(page_lens_kernel, dim3(1), dim3(64), 0, st, l, batch, lens, n_new, total);
+    return hipGetLastError();
+}
+
+hipError_t sum_sets(float* x, int ns, size_t n, hipStream_t st) {
+    if (ns <= 1) return hipSuccess;
+    hipLaunchKernelGGL(sum_sets_kernel, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, reinterpret_cast<f32x4*>(x), ns, n / 4);
+    return hipGetLastError();
+}
+
+}  // namespace msd
 
 extern "C" {
 
@@ -236,13 +277,7 @@ int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows
     if (((size_t)batch * KH + 7) * p.nsp * p.ncg > (size_t)INT32_MAX) return fail_global(METASD_E_INVALID, "attn_pages: too many requests, heads and rows for one launch");
     const PagesAttn a{q, out, (size_t)q_ld, (size_t)out_ld, 0, table, start, lens, (float*)scratch, scale * 1.44269504088896341f, 0, batch, width, rows, n_heads, n_heads / KH,
                       max_new, p.spw, p.nsp, p.ncg};
-    const Pool pl = pool_of(*pages);
-    hipStream_t st = (hipStream_t)hip_stream;
-#define GO(HD) if (dtype == METASD_BF16) launch_attn<HD, 1>(a, pl, p, st); else launch_attn<HD, 3>(a, pl, p, st)
-    if (hd == 128) { GO(128); }
-    else if (hd == 64) { GO(64); }
-    else { GO(32); }
-#undef GO
+    launch_attn_any(*pages, dtype, a, p, (hipStream_t)hip_stream);
     if (hipGetLastError() != hipSuccess) return fail_global(METASD_E_HIP, "attn_pages: launch failed");
     return METASD_OK;
 }

@@ -27,7 +27,9 @@ struct PagesPlan {
 // iteration of its 512 positions takes 1.75 (head_dim 128; 64: 1.15) us with bf16 rows and 2.4 (1.7) with fp32 ones; the records, their merge
 // and its launch cost some 6.5.  Measured, alone / split: 32 heads of 128, 6 rows behind 1000 positions, fp32 11.6 / 15.0 us, 2000 16.9 / 14.8, bf16
 // 12.7 / 15.1, 4000 20.5 / 14.9; 192 heads of 64, bf16 rows behind 4000 16.5 / 20.0, fp32 behind 16000 66.5 / 61.2.
-inline PagesPlan plan_pages(int B, int KH, int G, int hd, int max_new, int max_len, int terms, int n_cu) {
+// limit: floats of records that there is room for.
+inline size_t pages_records(const PagesPlan& p, int B, int KH, int hd);
+inline PagesPlan plan_pages(int B, int KH, int G, int hd, int max_new, int max_len, int terms, int n_cu, size_t limit = SIZE_MAX) {
     PagesPlan p{};
     const long cols = (long)max_new * G;
     p.ct = cols <= 16 ? 1 : 2;
@@ -44,18 +46,22 @@ inline PagesPlan plan_pages(int B, int KH, int G, int hd, int max_new, int max_l
         const long wgs = (long)B * KH * p.ncg;
         int want = (int)std::max(1L, std::min(16L, 2L * n_cu / wgs));
         want = std::min(want, std::max(1, nsub / 8));
-        p.spw = 2 * ((nsub + 2 * want - 1) / (2 * want));
-        p.nsp = (nsub + p.spw - 1) / p.spw;
-        return p;
+        for (;; want /= 2) {
+            p.spw = 2 * ((nsub + 2 * want - 1) / (2 * want));
+            p.nsp = (nsub + p.spw - 1) / p.spw;
+            if (want == 1 || pages_records(p, B, KH, hd) <= limit) return p;
+        }
     }
     const long wgs = (long)B * KH * p.ncg;
     const double alone = (nsub + 15) / 16 * (hd == 128 ? (terms == 1 ? 1.75 : 2.4) : (terms == 1 ? 1.15 : 1.7));
     p.nw = p.ct == 1 && wgs <= n_cu && alone * (1.0 - (double)wgs / n_cu) <= 6.5 ? 16 : 4;
     int want = p.nw == 16 ? 1 : (int)std::max(1L, std::min(32L, (4L * n_cu + wgs - 1) / wgs));     // spans per context that fill the chip
     want = std::min(want, std::max(1, nsub / (2 * p.nw)));
-    p.spw = p.nw * ((nsub + p.nw * want - 1) / (p.nw * want));
-    p.nsp = (nsub + p.spw - 1) / p.spw;
-    return p;
+    for (;; want /= 2) {
+        p.spw = p.nw * ((nsub + p.nw * want - 1) / (p.nw * want));
+        p.nsp = (nsub + p.spw - 1) / p.spw;
+        if (want == 1 || pages_records(p, B, KH, hd) <= limit) return p;
+    }
 }
 
 // floats of the records: (O, maximum, sum) of every column and span, where there is more than one
