@@ -382,7 +382,8 @@ int32_t metasd_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page, si
  * last, and pages given back can be taken from the next call on.  All arrays are int32 on the device; table [batch][width], held [batch],
  * ring [n_pages] and state [4] are updated in place (a new pool: held = 0, ring = 0 .. n_pages - 1, state = {0, n_pages, 0, 0}).
  * Out: start [batch + 1], the first row of every request in a block of all new rows; slots [rows] and pos [rows], where each goes and its
- * position (slot -1: request not served; both -1: behind the last row); served [batch]. */
+ * position (slot -1: request not served; both -1: behind the last row); served [batch].  rows may be 0 (pages only go back).  A pool is used
+ * by one call at a time. */
 #define METASD_PLAN_MAX_BATCH 4096
 int32_t metasd_page_plan(int32_t* table, int32_t batch, int32_t width, int32_t* held, int32_t* ring, int32_t n_pages, int32_t* state,
                          const int32_t* lens, const int32_t* n_new, int32_t page, int32_t rows, int32_t* slots, int32_t* pos, int32_t* start,
@@ -409,7 +410,7 @@ typedef struct {
 
 /* Row r at position pos[r]: q rotated into q_out (which may be q itself), k rotated and v appended at slots[r] (slot -1, or outside the pool:
  * nothing is appended; the slots of a call differ from each other).  q and q_out may be NULL (nothing to rotate), or k, v and slots (nothing
- * to append; pages then only gives head_dim).  Angles are formed in 64 bits, the rotation in 32. */
+ * to append; pages then only gives head_dim).  rows <= 2^22.  Angles are formed in 64 bits, the rotation in 32. */
 int32_t metasd_rope_append(const metasd_rope* rope, const metasd_pages* pages, int32_t dtype, int32_t rows, int32_t n_heads, const void* q,
                            int64_t q_ld, void* q_out, int64_t q_out_ld, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
                            const int32_t* pos, const int32_t* slots, void* hip_stream);
@@ -421,7 +422,7 @@ int32_t metasd_kv_rows(const metasd_pages* pages, const int32_t* slots, int32_t 
  * positions, which all lie in its pages; row i of n sees the positions up to lens[b] - n + i (a row that sees none becomes zeros).  Query head h
  * reads K/V head h / (n_heads / n_kv_heads).  out = softmax(scale q K^T) V, rows behind the last request are left as they were.
  * max_new: the most rows a request has (further ones are not computed), max_len: about the longest context; both only bound the launch,
- * lengths are read on the device.  A table entry outside the pool is read as its last page.  bf16: weights are rounded to bf16 before the
+ * lengths are read on the device.  out is not q; rows <= 2^22.  A table entry outside the pool is read as its last page.  bf16: weights are rounded to bf16 before the
  * product with V; fp32: q and weights are taken as three bf16 terms, 24 bits; sums are in 32 bits.
  * scratch: metasd_attn_pages_scratch bytes for the same arguments on the same device (may be 0: NULL), used by one call at a time. */
 int32_t metasd_attn_pages_scratch(int32_t batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t max_new,
@@ -435,7 +436,7 @@ int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows
  * without a law (copied from a text), q = 1 at the draft and 0 elsewhere.  n_acc[b] = the first failure (a draft outside the vocabulary
  * fails), else n_draft[b].  The token after it is drawn by inverse CDF with w[b] - the smallest v whose sum of weights up to v exceeds w[b]
  * times their sum - from max(0, P - Q) at the failure (P itself if that is zero everywhere), or from P[b][n_draft[b]]; -1 if no weight is
- * positive.  Weights need not sum to one; what is not above zero, a NaN among them, counts as zero.  Sums are in 64 bits.
+ * positive.  u and w are in [0, 1).  Weights need not sum to one; what is not above zero, a NaN among them, counts as zero.  Sums are in 64 bits.
  * P [rows][gamma + 1][V]: elements (b, j, v) at b * p_row + j * p_pos + v; Q the same; d [rows][gamma], u [rows][gamma], w [rows].
  * Out: n_acc [rows], tokens [rows][gamma + 1]: the accepted drafts, the drawn token, -1 behind it. */
 #define METASD_ACCEPT_PROBS_MAX_VOCAB (1 << 20)

@@ -564,12 +564,14 @@ def rope_append(q, k, v, pos: torch.Tensor, slots, pool, page: int, n_kv_heads: 
     lead = q if q is not None else k
     st = _on(lead, (pos,) if k is None else (pos, slots))
     rows = lead.shape[0]
+    if rows == 0:                                       # nothing to do
+        return out if out is not None or q is None else q.new_empty((0, q.shape[1] if q.dim() == 3 else q.shape[1] // head_dim, head_dim))
     if pos.numel() != rows or (k is not None and slots.numel() != rows):
         raise ValueError("rope_append: one position and one slot per row")
     H = ldq = ldo = ldk = ldv = 0
     if q is not None:
         ldq = _rows3("q", q, rows, None, head_dim, q)
-        H = q.numel() // (rows * head_dim) if rows else 0
+        H = q.numel() // (rows * head_dim)
         if out is None:
             out = torch.empty((rows, H, head_dim), dtype=q.dtype, device=q.device)
         ldo = _rows3("out", out, rows, H, head_dim, q)
@@ -592,6 +594,8 @@ def kv_rows(pool: torch.Tensor, slots: torch.Tensor, page: int, n_kv_heads: int,
     pages = _pages(pool, page, n_kv_heads, head_dim)
     rows, dev = slots.numel(), pool.device
     k, v = torch.empty((rows, n_kv_heads, head_dim), dtype=dtype, device=dev), torch.empty((rows, n_kv_heads, head_dim), dtype=dtype, device=dev)
+    if rows == 0:
+        return k, v
     _check(load_library().metasd_kv_rows(C.byref(pages), slots.data_ptr(), rows, _DTYPES.get(dtype, -1), k.data_ptr(), v.data_ptr(), st))
     return k, v
 
@@ -614,6 +618,8 @@ def attn_pages(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, start: 
         raise ValueError("attn_pages: start has batch + 1 entries, lens batch, the pool is on the same device")
     if out is None:
         out = torch.empty((rows, H, hd), dtype=q.dtype, device=q.device)
+    if rows == 0:
+        return out
     dt = _DTYPES.get(q.dtype, -1)
     ldq, ldo = _rows3("q", q, rows, H, hd, q), _rows3("out", out, rows, H, hd, q)
     pages = _pages(pool, page, n_kv_heads, hd)
@@ -644,6 +650,8 @@ def accept_probs(P: torch.Tensor, Q, d: torch.Tensor, n_draft, u: torch.Tensor, 
         _on(P, (n_acc, tokens))
         if n_acc.numel() < rows or tokens.numel() < rows * g1:
             raise ValueError("accept_probs: out is too small")
+    if rows == 0:
+        return out
     ps, qs = P.stride(), (0, 0) if Q is None else Q.stride()
     _check(load_library().metasd_accept_probs(P.data_ptr(), ps[0], ps[1], None if Q is None else Q.data_ptr(), qs[0], qs[1], d.data_ptr(),
                                               None if n_draft is None else n_draft.data_ptr(), u.data_ptr(), w.data_ptr(), rows, g1 - 1, V, n_acc.data_ptr(),

@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -13,6 +14,9 @@
 using namespace msd;
 
 namespace {
+
+// Rows of a call: a launch holds fewer than 2^32 work-items (1024 a row at most), and rows times heads of a group stay within 31 bits.
+constexpr int MAX_LAUNCH_ROWS = 1 << 22;
 
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
 size_t tile_bytes(int hd) { return (size_t)17 * hd; }
@@ -128,6 +132,8 @@ const char* check_attn(int32_t batch, int32_t n_heads, int32_t KH, int32_t hd, i
     if (batch < 1 || batch > 65535) return "batch must be 1..65535";
     if (!shape_ok(KH, hd, 16) || n_heads < 1 || n_heads % KH || n_heads / KH > 256) return "n_heads must be a multiple of n_kv_heads (up to 256 times), head_dim 32, 64 or 128";
     if (max_new < 1 || max_new > (1 << 20) || max_len < 1) return "max_new must be 1..2^20, max_len positive";
+    // at most 2^23 workgroups of 256 (a launch holds fewer than 2^32 work-items), and 2^26 columns for the merge
+    if ((int64_t)batch * KH > (1 << 22) || (int64_t)batch * n_heads * max_new > (1 << 26)) return "too much for one launch: batch * n_kv_heads <= 2^22, batch * n_heads * max_new <= 2^26";
     return nullptr;
 }
 
@@ -175,14 +181,14 @@ int32_t metasd_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page, si
 
 int32_t metasd_page_plan(int32_t* table, int32_t batch, int32_t width, int32_t* held, int32_t* ring, int32_t n_pages, int32_t* state, const int32_t* lens,
                          const int32_t* n_new, int32_t page, int32_t rows, int32_t* slots, int32_t* pos, int32_t* start, int32_t* served, void* hip_stream) {
-    if (!table || !held || !ring || !state || !lens || !n_new || !slots || !pos || !start || !served) return fail_global(METASD_E_INVALID, "page_plan: NULL pointer");
+    if (!table || !held || !ring || !state || !lens || !n_new || (rows > 0 && (!slots || !pos)) || !start || !served) return fail_global(METASD_E_INVALID, "page_plan: NULL pointer");
     if (batch < 1 || batch > METASD_PLAN_MAX_BATCH || width < 1 || (int64_t)batch * width > INT32_MAX) return fail_global(METASD_E_INVALID, "page_plan: batch 1..%d, width >= 1, batch * width within 31 bits", METASD_PLAN_MAX_BATCH);
     if (!shape_ok(1, 32, page)) return fail_global(METASD_E_INVALID, "page_plan: page must be a power of two from 16 to 1024");
     if (n_pages < 1 || (int64_t)n_pages * page > INT32_MAX) return fail_global(METASD_E_INVALID, "page_plan: n_pages * page must be within 31 bits");
-    if (rows < 1 || rows > (1 << 30)) return fail_global(METASD_E_INVALID, "page_plan: rows must be 1..2^30");
+    if (rows < 0 || rows > (1 << 30)) return fail_global(METASD_E_INVALID, "page_plan: rows must be 0..2^30");
     static_assert(METASD_PLAN_MAX_BATCH == PLAN_BATCH, "requests of a plan");
     const PlanArgs a{table, held, ring, state, lens, n_new, slots, pos, start, served, batch, width, n_pages, shift_of(page), rows};
-    hipLaunchKernelGGL(page_plan_kernel, dim3((rows + PLAN_NT - 1) / PLAN_NT), dim3(PLAN_NT), 0, (hipStream_t)hip_stream, a);
+    hipLaunchKernelGGL(page_plan_kernel, dim3(std::max(1, (rows + PLAN_NT - 1) / PLAN_NT)), dim3(PLAN_NT), 0, (hipStream_t)hip_stream, a);
     if (hipGetLastError() != hipSuccess) return fail_global(METASD_E_HIP, "page_plan: launch failed");
     return METASD_OK;
 }
@@ -193,13 +199,14 @@ int32_t metasd_rope_append(const metasd_rope* rope, const metasd_pages* pages, i
     if (const char* bad = check_pages(pages, k != nullptr)) return fail_global(METASD_E_INVALID, "rope_append: %s", bad);
     if (!rope || !pos || (!q && !k) || !q != !q_out || !k != !v || (k && !slots)) return fail_global(METASD_E_INVALID, "rope_append: NULL pointer (q and q_out, or k, v and slots, may be NULL together)");
     if (dtype != METASD_F32 && dtype != METASD_BF16) return fail_global(METASD_E_INVALID, "rope_append: dtype");
-    if (rows < 1 || rows > (1 << 30) || (q && (n_heads < 1 || n_heads > 65535))) return fail_global(METASD_E_INVALID, "rope_append: rows 1..2^30, n_heads 1..65535");
+    if (rows < 1 || rows > MAX_LAUNCH_ROWS || (q && (n_heads < 1 || n_heads > 65535))) return fail_global(METASD_E_INVALID, "rope_append: rows 1..2^22, n_heads 1..65535");
     if (const char* bad = check_rope(*rope, pages->head_dim)) return fail_global(METASD_E_INVALID, "rope_append: %s", bad);
     const int hd = pages->head_dim;
     const size_t es = dtype == METASD_BF16 ? 2 : 4;
     const char* bad = nullptr;
     if (q) { check_rows("q", q, q_ld, (int64_t)n_heads * hd, es, &bad); check_rows("q_out", q_out, q_out_ld, (int64_t)n_heads * hd, es, &bad); }
     if (k) { check_rows("k", k, k_ld, (int64_t)pages->n_kv_heads * hd, es, &bad); check_rows("v", v, v_ld, (int64_t)pages->n_kv_heads * hd, es, &bad); }
+    if (q == q_out && q && q_ld != q_out_ld) bad = "q_out";
     if (bad) return fail_global(METASD_E_INVALID, "rope_append: rows of %s must start on 16 bytes and not overlap", bad);
     // the table of the last description is kept per thread: its powers cost more than the launch
     thread_local metasd_rope have{};
@@ -261,20 +268,20 @@ int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows
     if (dtype != METASD_F32 && dtype != METASD_BF16) return fail_global(METASD_E_INVALID, "attn_pages: dtype");
     const int hd = pages->head_dim, KH = pages->n_kv_heads;
     if (const char* bad = check_attn(batch, n_heads, KH, hd, max_new, max_len)) return fail_global(METASD_E_INVALID, "attn_pages: %s", bad);
-    if (rows < 1 || rows > (1 << 30) || width < 1 || (int64_t)batch * width > INT32_MAX || (int64_t)width * pages->page > INT32_MAX)
-        return fail_global(METASD_E_INVALID, "attn_pages: rows 1..2^30, width >= 1, batch * width and width * page within 31 bits");
+    if (rows < 1 || rows > MAX_LAUNCH_ROWS || width < 1 || (int64_t)batch * width > INT32_MAX || (int64_t)width * pages->page > INT32_MAX)
+        return fail_global(METASD_E_INVALID, "attn_pages: rows 1..2^22, width >= 1, batch * width and width * page within 31 bits");
     if (!(scale > 0.f) || !std::isfinite(scale)) return fail_global(METASD_E_INVALID, "attn_pages: scale must be positive");
     const char* bad = nullptr;
     const size_t es = dtype == METASD_BF16 ? 2 : 4;
     check_rows("q", q, q_ld, (int64_t)n_heads * hd, es, &bad);
     check_rows("out", out, out_ld, (int64_t)n_heads * hd, es, &bad);
+    if (q == out) bad = "out (which is q)";
     if (bad) return fail_global(METASD_E_INVALID, "attn_pages: rows of %s must start on 16 bytes and not overlap", bad);
     const int n_cu = n_cu_of_device();
     if (!n_cu) return fail_global(METASD_E_HIP, "attn_pages: cannot query the device");
     const PagesPlan p = plan_pages(batch, KH, n_heads / KH, hd, max_new, max_len, dtype == METASD_BF16 ? 1 : 2, n_cu);
     const size_t need = pages_records(p, batch, KH, hd) * sizeof(float);
     if (need && (!scratch || !aligned(scratch) || scratch_bytes < need)) return fail_global(METASD_E_WORKSPACE, "attn_pages: scratch of %zu bytes, 16-byte aligned, needed (metasd_attn_pages_scratch)", need);
-    if (((size_t)batch * KH + 7) * p.nsp * p.ncg > (size_t)INT32_MAX) return fail_global(METASD_E_INVALID, "attn_pages: too many requests, heads and rows for one launch");
     const PagesAttn a{q, out, (size_t)q_ld, (size_t)out_ld, 0, table, start, lens, (float*)scratch, scale * 1.44269504088896341f, 0, batch, width, rows, n_heads, n_heads / KH,
                       max_new, p.spw, p.nsp, p.ncg};
     launch_attn_any(*pages, dtype, a, p, (hipStream_t)hip_stream);
@@ -285,8 +292,8 @@ int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows
 int32_t metasd_accept_probs(const float* P, int64_t p_row, int64_t p_pos, const float* Q, int64_t q_row, int64_t q_pos, const int32_t* d, const int32_t* n_draft,
                             const float* u, const float* w, int32_t rows, int32_t gamma, int32_t V, int32_t* n_acc, int32_t* tokens, void* hip_stream) {
     if (!P || !d || !u || !w || !n_acc || !tokens) return fail_global(METASD_E_INVALID, "accept_probs: NULL pointer (Q and n_draft may be NULL)");
-    if (rows < 1 || rows > (1 << 24) || gamma < 1 || gamma > 1024 || V < 1 || V > METASD_ACCEPT_PROBS_MAX_VOCAB)
-        return fail_global(METASD_E_INVALID, "accept_probs: rows 1..2^24, gamma 1..1024, V 1..%d", METASD_ACCEPT_PROBS_MAX_VOCAB);
+    if (rows < 1 || rows > MAX_LAUNCH_ROWS / 2 || gamma < 1 || gamma > 1024 || V < 1 || V > METASD_ACCEPT_PROBS_MAX_VOCAB)
+        return fail_global(METASD_E_INVALID, "accept_probs: rows 1..2^21, gamma 1..1024, V 1..%d", METASD_ACCEPT_PROBS_MAX_VOCAB);
     if (p_pos < V || (rows > 1 && p_row < V) || (Q && (q_pos < V || (rows > 1 && q_row < V)))) return fail_global(METASD_E_INVALID, "accept_probs: rows of probabilities must not overlap");
     const int vec = aligned(P) && p_row % 4 == 0 && p_pos % 4 == 0 && (!Q || (aligned(Q) && q_row % 4 == 0 && q_pos % 4 == 0));
     const AcceptProbs a{P, Q, (size_t)p_row, (size_t)p_pos, (size_t)q_row, (size_t)q_pos, d, n_draft, u, w, gamma, V, vec, n_acc, tokens};

@@ -86,6 +86,24 @@ def test_plan_serves_later_requests_that_need_nothing():
     assert out["served"].tolist() == [1, 0, 1, 0]
 
 
+def test_plan_without_rows_only_gives_back():
+    h = plan_state(np.random.default_rng(6), 3, 4, 12, 16, [3, 1, 2])
+    g = [dev(x) for x in h]
+    out = check_plan(g, h, [16, 0, 32], [0, 0, 0], 16, 0)
+    assert out["slots"].numel() == 0 and g[1].tolist() == [1, 0, 2]
+
+
+def test_nothing_to_do():
+    """Calls without rows return without a launch."""
+    pool, _ = new_pool(1, 2, 64, 16)
+    none = torch.zeros(0, dtype=torch.int32, device=DEV)
+    q = torch.zeros((0, 4, 64), device=DEV)
+    k = torch.zeros((0, 2, 64), device=DEV)
+    assert M.rope_append(q, k, k, none, none, pool, 16, 2, 64, M.Rope("half", 64)).shape == (0, 4, 64)
+    assert M.kv_rows(pool, none, 16, 2, 64)[0].shape == (0, 2, 64)
+    assert M.attn_pages(q, pool, dev([[0]]), dev([0, 0]), dev([0]), 16, 2, 1.0, 1, 1).shape == (0, 4, 64)
+
+
 # ---- rotation and append
 
 def new_pool(n_pages, KH, hd, page, pad=0, fill=0xA5):

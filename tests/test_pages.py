@@ -41,7 +41,7 @@ def test_page_bytes(lib):
 
 
 @pytest.mark.parametrize("kw,text", [(dict(batch=0), "batch"), (dict(batch=4097), "batch"), (dict(width=0), "width"), (dict(batch=4096, width=1 << 20), "31 bits"), (dict(page=17), "power of two"),
-                                     (dict(n_pages=0), "n_pages"), (dict(n_pages=1 << 27), "31 bits"), (dict(rows=0), "rows"), (dict(null=5), "NULL")])
+                                     (dict(n_pages=0), "n_pages"), (dict(n_pages=1 << 27), "31 bits"), (dict(rows=-1), "rows"), (dict(null=5), "NULL"), (dict(null=6), "NULL")])
 def test_plan_refusals(lib, kw, text):
     a = dict(batch=2, width=4, n_pages=8, page=16, rows=8, null=None)
     a.update(kw)
@@ -61,12 +61,13 @@ def test_bad_pages_are_refused(lib, kw, text):
     r = M.Rope("half", 64)
     refused(lib, lib.metasd_rope_append(C.byref(r.c), C.byref(p), 0, 4, 2, OK, 128, OK, 128, OK, 128, OK, 128, OK, OK, None), text)
     refused(lib, lib.metasd_kv_rows(C.byref(p), OK, 4, 0, OK, OK, None), text)
-    refused(lib, lib.metasd_attn_pages(C.byref(p), 0, 4, 2, OK, 128, OK, 128, OK, 2, 3, OK, OK, 4, 40, 1.0, OK, 1 << 30, None), text)
+    refused(lib, lib.metasd_attn_pages(C.byref(p), 0, 4, 2, OK, 128, 2 * OK, 128, OK, 2, 3, OK, OK, 4, 40, 1.0, OK, 1 << 30, None), text)
 
 
 @pytest.mark.parametrize("kw,text", [(dict(q=None), "NULL"), (dict(v=None), "NULL"), (dict(slots=None), "NULL"), (dict(pos=None), "NULL"), (dict(q=None, q_out=None, k=None, v=None), "NULL"),
                                      (dict(dtype=2), "dtype"), (dict(rows=0), "rows"), (dict(H=0), "n_heads"), (dict(q=OK + 4), "rows of q"), (dict(q_ld=127), "rows of q"),
-                                     (dict(q_ld=130), "rows of q"), (dict(q_out_ld=64), "rows of q_out"), (dict(k=OK + 8), "rows of k"), (dict(v_ld=64), "rows of v")])
+                                     (dict(q_ld=130), "rows of q"), (dict(q_out_ld=64), "rows of q_out"), (dict(k=OK + 8), "rows of k"), (dict(v_ld=64), "rows of v"),
+                                     (dict(rows=(1 << 22) + 1), "rows"), (dict(q_out_ld=256), "rows of q_out")])
 def test_append_refusals(lib, kw, text):
     a = dict(dtype=0, rows=4, H=2, q=OK, q_ld=128, q_out=OK, q_out_ld=128, k=OK, k_ld=128, v=OK, v_ld=128, pos=OK, slots=OK)
     a.update(kw)
@@ -88,9 +89,10 @@ def test_rope_refusals(lib, kw, text):
 
 @pytest.mark.parametrize("kw,text", [(dict(q=None), "NULL"), (dict(lens=None), "NULL"), (dict(dtype=3), "dtype"), (dict(rows=0), "rows"), (dict(H=3), "n_heads"), (dict(batch=0), "batch"),
                                      (dict(batch=65536), "batch"), (dict(width=0), "width"), (dict(width=1 << 28), "31 bits"), (dict(max_new=0), "max_new"), (dict(max_len=0), "max_len"),
-                                     (dict(scale=0.0), "scale"), (dict(scale=math.nan), "scale"), (dict(q_ld=129), "rows of q"), (dict(out=OK + 4), "rows of out")])
+                                     (dict(scale=0.0), "scale"), (dict(scale=math.nan), "scale"), (dict(q_ld=129), "rows of q"), (dict(out=OK + 4), "rows of out"), (dict(out=OK), "which is q"),
+                                     (dict(rows=(1 << 22) + 1), "rows"), (dict(batch=65535, max_new=1 << 14), "one launch")])
 def test_attention_refusals(lib, kw, text):
-    a = dict(dtype=0, rows=4, H=2, q=OK, q_ld=128, out=OK, out_ld=128, table=OK, batch=2, width=3, start=OK, lens=OK, max_new=2, max_len=40, scale=1.0)
+    a = dict(dtype=0, rows=4, H=2, q=OK, q_ld=128, out=2 * OK, out_ld=128, table=OK, batch=2, width=3, start=OK, lens=OK, max_new=2, max_len=40, scale=1.0)
     a.update(kw)
     refused(lib, lib.metasd_attn_pages(C.byref(pages()), a["dtype"], a["rows"], a["H"], a["q"], a["q_ld"], a["out"], a["out_ld"], a["table"], a["batch"], a["width"], a["start"], a["lens"],
                                        a["max_new"], a["max_len"], a["scale"], OK, 1 << 30, None), text)
