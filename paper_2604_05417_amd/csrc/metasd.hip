@@ -1772,9 +1772,16 @@ int forward_segs_step(metasd_ctx* c, Model& M, const Segs& sg, float* logits, in
     int rc;
     hipLaunchKernelGGL(embed_seg_kernel<T>, dim3(R), dim3(256), 0, st, (const int32_t*)c->d_hist(), c->cfg.max_ctx, (const T*)M.w[0], D, h, sg);
     LAUNCH_CHECK(c, "embed (segments)");
-    hipLaunchKernelGGL(rope_table_seg_kernel, dim3(R), dim3(hd / 2), 0, st, sg, hd, d.rope_theta, c->d_rope(), rowkv,
-                       (size_t)M.kv_layers * 2 * d.n_kv_heads * c->cfg.max_ctx * hd);
-    LAUNCH_CHECK(c, "rope_table (segments)");
+    const int DKV = d.n_kv_heads * hd;
+    int max_len = 1;
+    for (int s = 0; s < sg.n; ++s) max_len = std::max(max_len, sg.pos0[s] + sg.m[s]);
+    if (M.paged.on()) {
+        if ((rc = plan_paged(c, M, sg))) return rc;
+    } else {
+        hipLaunchKernelGGL(rope_table_seg_kernel, dim3(R), dim3(hd / 2), 0, st, sg, hd, d.rope_theta, c->d_rope(), rowkv,
+                           (size_t)M.kv_layers * 2 * d.n_kv_heads * c->cfg.max_ctx * hd);
+        LAUNCH_CHECK(c, "rope_table (segments)");
+    }
     auto norm_in = [&](const void* gain) {
         StepArgs a{};
         a.h = h; a.gain = (const bf16_t*)gain; a.eps = d.rms_eps; a.m = R; a.K = D;
@@ -1783,9 +1790,16 @@ int forward_segs_step(metasd_ctx* c, Model& M, const Segs& sg, float* logits, in
     const SegAttn at = plan_segs(c, d, hd, sg);
     for (int L = 0; L < d.n_layers; ++L) {
         StepArgs a = norm_in(M.layer_w(L, 0));
-        a.rowkv = rowkv;
-        if ((rc = gemm_step_qkv(c, M, L, 0, a))) return rc;
-        if ((rc = attention_seg<T>(c, M, L, sg, at))) return rc;
+        if (M.paged.on()) {
+            a.out = c->d_part(); a.N = DQ + 2 * DKV;
+            if ((rc = gemm_step_norm<STEP_OUT, false>(c, a, M.layer_w(L, 1), DQ, M.layer_w(L, 2), DKV, M.layer_w(L, 3), DKV))) return rc;
+            if ((rc = paged_append(c, M, L, R, 1))) return rc;
+            if ((rc = paged_attention(c, M, L, R, sg.ms, max_len))) return rc;
+        } else {
+            a.rowkv = rowkv;
+            if ((rc = gemm_step_qkv(c, M, L, 0, a))) return rc;
+            if ((rc = attention_seg<T>(c, M, L, sg, at))) return rc;
+        }
         if ((rc = residual_add(c, c->d_ao(), R, DQ, M.layer_w(L, 4), D, h, M.layer_w(L, 5)))) return rc;
         a = norm_in(M.layer_w(L, 5));
         a.out = (float*)c->d_act(); a.N = F; a.swiglu = d.act == METASD_SWIGLU;
@@ -1897,7 +1911,7 @@ int forward_segs(metasd_ctx* c, Model& M, const Segs& sg, float* logits, int out
     for (int s = 0; s < sg.n; ++s)
         if (sg.pos0[s] + sg.m[s] > c->cfg.max_ctx)
             return c->fail(METASD_E_OVERFLOW, "sequence %d: positions %d..%d exceed max_ctx %d", sg.seq[s], sg.pos0[s], sg.pos0[s] + sg.m[s], c->cfg.max_ctx);
-    if (!M.paged.on() && segs_step_ok(c, M, sg.n * sg.ms)) return forward_segs_step(c, M, sg, logits, out_seq_rows, out_row0, last_only);
+    if (segs_step_ok(c, M, sg.n * sg.ms)) return forward_segs_step(c, M, sg, logits, out_seq_rows, out_row0, last_only);
     if (M.d.dtype == METASD_BF16) return forward_segs_t<bf16_t>(c, M, sg, logits, out_seq_rows, out_row0, last_only);
     return forward_segs_t<float>(c, M, sg, logits, out_seq_rows, out_row0, last_only);
 }
