@@ -547,7 +547,7 @@ def page_plan(table: torch.Tensor, held: torch.Tensor, ring: torch.Tensor, state
         raise ValueError("page_plan: held, lens and n_new have one entry per request, state four")
     if out is None:
         buf = torch.empty(2 * rows + 2 * B + 1, dtype=torch.int32, device=table.device)
-        slots, pos, start, served = buf.split((rows, rows, B + 1, B))
+        slots, pos, start, served = torch.split_with_sizes(buf, (rows, rows, B + 1, B))
         out = dict(slots=slots, pos=pos, start=start, served=served)
     else:
         _on(table, (out["slots"], out["pos"], out["start"], out["served"]))

@@ -33,12 +33,12 @@ __device__ __forceinline__ unsigned char* tile_at(const Pool& pl, int page, int 
 }
 
 // ------------------------------------------------------------------------------------------
-// Block tables and slots.  One workgroup does everything for its 1024 rows: every workgroup sums the requests' rows and pages for itself (at
+// Block tables and slots.  A workgroup does everything for a row per thread: every workgroup sums the requests' rows and pages for itself (at
 // most PLAN_BATCH of them, 20 bytes each, from L2), so that nothing has to be handed from one to another; the pages that change hands are
 // dealt out over all of them.  Pages are taken from the front of the ring and given back behind its last, two stretches that do not meet
 // because the ring has room for every page there is.  The counts of the state and of the requests are read by all and written by the
 // workgroup that comes to its end last.
-constexpr int PLAN_NT = 1024, PLAN_BATCH = 4096, PLAN_PER = PLAN_BATCH / PLAN_NT;
+constexpr int PLAN_BATCH = 4096, PLAN_PER = 4;      // requests of a call, and of a thread
 
 struct PlanArgs {
     int *table, *held, *ring, *state;
@@ -48,7 +48,7 @@ struct PlanArgs {
 };
 
 // Inclusive sum over the workgroup of one value per thread; *total: of all.
-template <typename T>
+template <int NT, typename T>
 __device__ __forceinline__ T block_scan(T v, T* wave_tot, T* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -61,7 +61,7 @@ __device__ __forceinline__ T block_scan(T v, T* wave_tot, T* total) {
     __syncthreads();
     T before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < PLAN_NT / 64; ++w) {
+    for (int w = 0; w < NT / 64; ++w) {
         const T x = wave_tot[w];
         before += w < wave ? x : (T)0;
         all += x;
@@ -80,12 +80,13 @@ __device__ __forceinline__ int first_above(const int* end, int n, int x) {
     return lo;
 }
 
-__global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
-    __shared__ int row_end[PLAN_BATCH], take_end[PLAN_BATCH], back_end[PLAN_BATCH];
-    __shared__ long long tot64[PLAN_NT / 64];
-    __shared__ int tot32[PLAN_NT / 64];
+template <int NT>
+__global__ __launch_bounds__(NT) void page_plan_kernel(PlanArgs a) {
+    __shared__ int row_end[NT * PLAN_PER], take_end[NT * PLAN_PER], back_end[NT * PLAN_PER];
+    __shared__ long long tot64[NT / 64];
+    __shared__ int tot32[NT / 64];
     __shared__ int last;
-    const int tid = threadIdx.x, per = (a.B + PLAN_NT - 1) / PLAN_NT, b0 = tid * per;
+    const int tid = threadIdx.x, per = (a.B + NT - 1) / NT, b0 = tid * per;
     const int page = 1 << a.shift;
     int head = a.state[0] % a.n_pages, count = min(max(a.state[1], 0), a.n_pages);
     if (head < 0) head += a.n_pages;
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
         end[i] = sum;
     }
     long long all64;
-    const long long rows_before = block_scan<long long>(sum, tot64, &all64) - sum;
+    const long long rows_before = block_scan<NT>(sum, tot64, &all64) - sum;
     int t = 0, r = 0;
 #pragma unroll
     for (int i = 0; i < PLAN_PER; ++i) {
@@ -117,9 +118,9 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
         need[i] = fits ? need[i] : -need[i] - 1;       // (marked: not served whatever the ring holds)
     }
     int all_t, all_r;
-    int upto_t = block_scan<int>(t, tot32, &all_t) - t, upto_r = block_scan<int>(r, tot32, &all_r) - r;
+    int upto_t = block_scan<NT>(t, tot32, &all_t) - t, upto_r = block_scan<NT>(r, tot32, &all_r) - r;
     int new_held[PLAN_PER], served_to = 0;
-    __shared__ int taken_wave[PLAN_NT / 64];
+    __shared__ int taken_wave[NT / 64];
 #pragma unroll
     for (int i = 0; i < PLAN_PER; ++i) {
         if (i >= per) break;
@@ -143,10 +144,10 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
     __syncthreads();
     int taken = 0;
 #pragma unroll
-    for (int w = 0; w < PLAN_NT / 64; ++w) taken = max(taken, taken_wave[w]);
+    for (int w = 0; w < NT / 64; ++w) taken = max(taken, taken_wave[w]);
     auto upto = [&](int b) { const int x = take_end[b]; return x < 0 ? -x - 1 : x; };
     // ---- rows
-    const int r0 = blockIdx.x * PLAN_NT + tid;
+    const int r0 = blockIdx.x * NT + tid;
     if (r0 < a.rows) {
         int slot = -1, p = -1;
         const int b = first_above(row_end, a.B, r0);
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
         a.pos[r0] = p;
     }
     // ---- pages that change hands
-    const int grid = gridDim.x * PLAN_NT;
+    const int grid = gridDim.x * NT;
     for (int i = r0; i < taken; i += grid) {
         int lo = 0, hi = a.B;
         while (lo < hi) { const int mid = (lo + hi) >> 1; if (upto(mid) > i) hi = mid; else lo = mid + 1; }
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(PlanArgs a) {
         a.ring[(int)(((long long)head + count + i) % a.n_pages)] = a.table[(size_t)b * a.width + nd + (i - before)];
     }
     if (blockIdx.x == 0)
-        for (int b = tid; b <= a.B; b += PLAN_NT) {
+        for (int b = tid; b <= a.B; b += NT) {
             a.start[b] = b ? row_end[b - 1] : 0;
             if (b < a.B) a.served[b] = take_end[b] >= 0;
         }

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -37,9 +38,15 @@ const char* check_pages(const metasd_pages* p, bool pool) {
 }
 Pool pool_of(const metasd_pages& p) { return Pool{(unsigned char*)p.pool, p.page_stride, p.n_pages, shift_of(p.page), p.n_kv_heads}; }
 
+// CUs of the current device, 0 if it cannot be asked; asked for once per device
 int n_cu_of_device() {
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return 0;
+    constexpr int MAX_DEV = 64;
+    static std::atomic<int> known[MAX_DEV];
+    int dev = -1, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 0;
+    if (dev < MAX_DEV && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return 0;
+    if (dev < MAX_DEV) known[dev].store(n, std::memory_order_relaxed);
     return n;
 }
 
@@ -188,7 +195,13 @@ int32_t metasd_page_plan(int32_t* table, int32_t batch, int32_t width, int32_t* 
     if (rows < 0 || rows > (1 << 30)) return fail_global(METASD_E_INVALID, "page_plan: rows must be 0..2^30");
     static_assert(METASD_PLAN_MAX_BATCH == PLAN_BATCH, "requests of a plan");
     const PlanArgs a{table, held, ring, state, lens, n_new, slots, pos, start, served, batch, width, n_pages, shift_of(page), rows};
-    hipLaunchKernelGGL(page_plan_kernel, dim3(std::max(1, (rows + PLAN_NT - 1) / PLAN_NT)), dim3(PLAN_NT), 0, (hipStream_t)hip_stream, a);
+    hipStream_t st = (hipStream_t)hip_stream;
+#define GO(NT) hipLaunchKernelGGL((page_plan_kernel<NT>), dim3(std::max(1, (rows + NT - 1) / NT)), dim3(NT), 0, st, a)
+    // A call of few requests and few rows is bound by its barriers: four wavefronts meet sooner than
+    // sixteen (64 requests, 256 rows: 4.2 us against 5.6). Sixteen repeat the scan over the requests
+    // for fewer groups of rows (122 000 rows: 8.5 us against 11.4 with four).
+    if (batch <= 256 * PLAN_PER && rows <= 1024) GO(256); else GO(1024);
+#undef GO
     if (hipGetLastError() != hipSuccess) return fail_global(METASD_E_HIP, "page_plan: launch failed");
     return METASD_OK;
 }

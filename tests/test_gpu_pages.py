@@ -64,6 +64,20 @@ def test_plan_rounds(B, page, width, n_pages, most):
         lens[rng.random(B) < 0.2] = 0
 
 
+@pytest.mark.parametrize("B,rows", [(256, 1024), (257, 1023), (1024, 1024), (1024, 1025), (1023, 257), (1025, 1024), (1025, 300)])
+def test_plan_on_both_sides_of_its_forms(B, rows):
+    """Few requests and rows go to workgroups of 256 threads, others to 1024: the border, several requests of a thread, several workgroups."""
+    rng = np.random.default_rng(B + rows)
+    h = plan_state(rng, B, 4, 3 * B, 16)
+    g = [dev(x) for x in h]
+    lens = np.zeros(B, np.int64)
+    for step in range(4):
+        n_new = rng.integers(0, 12, B) * (rng.random(B) < min(1.0, rows / (4 * B)))
+        check_plan(g, h, lens, n_new, 16, rows)
+        lens = np.minimum(np.minimum(h[1] * 16, lens + n_new), 50)
+        lens[rng.random(B) < 0.3] = 0
+
+
 @pytest.mark.parametrize("lens,n_new,held,rows", [([0], [0], [0], 5), ([0], [1], [0], 1), ([5], [0], [1], 2), ([15], [1], [1], 1), ([16], [1], [1], 1), ([40], [3], [6], 3),
                                                   ([-4, 3], [2, -5], [0, 1], 4), ([0, 0, 0], [9, 1, 200], [0, 0, 0], 64), ([2 ** 31 - 1, 1], [2 ** 31 - 1, 3], [2, 0], 9)])
 def test_plan_edges(lens, n_new, held, rows):
