@@ -392,20 +392,25 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
 // The same for long blocks (prompts): every one of the four wavefronts has 16 columns of its own and all walk the same positions, 64 at a time.
 // Each widens one tile of 16 positions into LDS as the operands that all of them multiply with, so that a position is widened once for 64
 // columns; while they multiply, the codes of the next 64 are on their way.  One buffer, so that four workgroups share a CU: with two
-// buffers and half as many 56 instead of 44 us (1500 rows, 32 heads of 128, bf16), with 32 columns a wavefront 55, with a second team of four for
+// buffers and half as many 56 instead of 44 us (in the order of pairs; 1500 rows, 32 heads of 128, bf16), with 32 columns a wavefront 55, with a second team of four for
 // every other step 46; the kernel above, which widens for 32 columns, 51.  What bounds it: nearly as many cycles in LDS (32 KiB read per
 // wavefront and step, 1024) as in the exponentials and the widening (800) and in the products (512).
 // LDS layout: [K: tile][chunk][lane] and [V: pair of tiles][chunk][even, odd][lane], 16 bytes a lane.
-// Workgroup ids deal the (request, K/V head) pairs out over the 8 XCDs, so that the column groups of one share an L2, longest first.
+// Workgroup ids deal the (request, K/V head) pairs out over the 8 XCDs, so that the column groups of one share an L2.  Within a bundle of pairs
+// (512 workgroups or more) the longest groups come first, and every other round over the XCD's 32 CUs goes backwards: a CU that got the
+// longest group of one round gets the shortest of the next.  Pair after pair / so: prompts of 1500 rows 45.6 / 39.4 us, 4000 193 / 174, 8000 630 / 580, eight
+// requests of up to 500 rows behind up to 3000 positions 89 / 64 (bf16, 32 heads of 128); bundles of 128 workgroups lose 4 - 15 % of it.
 template <int HD, int TERMS>
 __global__ __launch_bounds__(256, TERMS == 1 ? 4 : 3) void attn_pages_long_kernel(PagesAttn a, Pool pl) {
     constexpr int KC = HD / 32, OS = HD + 4, GC = 64;  // columns of the workgroup
     __shared__ u32x4 k_sh[4][KC][64];
     __shared__ u32x4 v_sh[2][KC][2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-    const int y = blockIdx.x >> 3, per = a.ncg * a.nsp, unit = (blockIdx.x & 7) + 8 * (y / per), rest = y % per;
+    const int per = a.ncg * a.nsp, units = (int)(gridDim.x >> 3) / per, most = min(units, (511 + per) / per), y = blockIdx.x >> 3, bundle = y / (most * per);
+    const int n_units = min(most, units - bundle * most), z = y - bundle * most * per, round = z >> 5;
+    const int place = round & 1 ? min(32 * round + 31, n_units * per - 1) - (z & 31) : z, unit = (blockIdx.x & 7) + 8 * (bundle * most + place / a.nsp % n_units);
     if (unit >= a.B * pl.KH) return;                   // workgroup-uniform, as are the next two
-    const int cg = a.ncg - 1 - rest / a.nsp, sp = rest % a.nsp, b = unit / pl.KH, kh = unit - b * pl.KH;
+    const int cg = a.ncg - 1 - place / (a.nsp * n_units), sp = place % a.nsp, b = unit / pl.KH, kh = unit - b * pl.KH;
     const PagesReq rq = pages_req(a, b, pl.shift);
     const int ncol = rq.n * a.G;
     if (cg * GC >= ncol) return;

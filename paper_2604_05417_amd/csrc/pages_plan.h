@@ -7,8 +7,8 @@
 
 namespace msd {
 
-// Columns from which on a block takes the long form.  Without / with it, bf16 (fp32) rows: 1500 rows of 32 heads of 128 50.9 / 43.7 us (78.1 / 77.3), 700 29.1
-// / 20.7 (36.3 / 34.6), of 32 heads of 64 on 8 30.7 / 24.4 (48.6 / 41); 200 rows 10.8 / 11.8 (10.9 / 12.0); 128 behind 1872 positions 24.5 / 25.3 (27 / 31.8).
+// Columns from which on a block takes the long form.  Without / with it, bf16 (fp32) rows: 1500 rows of 32 heads of 128 50.9 / 39 us (78.1 / 60), 700 29.1
+// / 17.4 (36.3 / 27.6), of 32 heads of 64 on 8 30.7 / 24.4 (48.6 / 41); 200 rows 10.8 / 11.8 (10.9 / 12.0); 128 behind 1872 positions 24.5 / 25.3 (27 / 31.8).
 constexpr int PAGES_WIDE = 256;
 
 struct PagesPlan {
