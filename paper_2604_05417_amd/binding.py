@@ -562,6 +562,8 @@ def rope_append(q, k, v, pos: torch.Tensor, slots, pool, page: int, n_kv_heads: 
     """metasd_rope_append: q [rows, n_heads (,) head_dim] rotated (returned, [rows, n_heads, head_dim]); k rotated and v appended to the pool at
     `slots`.  q may be None, or k, v, slots and pool."""
     lead = q if q is not None else k
+    if lead is None or (k is not None and (v is None or slots is None or pool is None)):
+        raise ValueError("rope_append: q, or k with v, slots and pool, or both")
     st = _on(lead, (pos,) if k is None else (pos, slots))
     rows = lead.shape[0]
     if rows == 0:                                       # nothing to do
@@ -573,8 +575,9 @@ def rope_append(q, k, v, pos: torch.Tensor, slots, pool, page: int, n_kv_heads: 
         ldq = _rows3("q", q, rows, None, head_dim, q)
         H = q.numel() // (rows * head_dim)
         if out is None:
-            out = torch.empty((rows, H, head_dim), dtype=q.dtype, device=q.device)
-        ldo = _rows3("out", out, rows, H, head_dim, q)
+            out, ldo = torch.empty((rows, H, head_dim), dtype=q.dtype, device=q.device), H * head_dim
+        else:
+            ldo = _rows3("out", out, rows, H, head_dim, q)
     if k is not None:
         ldk, ldv = _rows3("k", k, rows, n_kv_heads, head_dim, lead), _rows3("v", v, rows, n_kv_heads, head_dim, lead)
         if pool.get_device() != lead.get_device():
@@ -582,9 +585,9 @@ def rope_append(q, k, v, pos: torch.Tensor, slots, pool, page: int, n_kv_heads: 
         pages = _pages(pool, page, n_kv_heads, head_dim)
     else:
         pages = _Pages(n_kv_heads, head_dim, page, 0, None, 0)
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    _check(load_library().metasd_rope_append(C.byref(rope.c), C.byref(pages), _DTYPES.get(lead.dtype, -1), rows, H, ptr(q), ldq, ptr(out) if q is not None else None, ldo, ptr(k), ldk,
-                                ptr(v), ldv, pos.data_ptr(), ptr(slots) if k is not None else None, st))
+    qp, op = (None, None) if q is None else (q.data_ptr(), out.data_ptr())
+    kp, vp, sp = (None, None, None) if k is None else (k.data_ptr(), v.data_ptr(), slots.data_ptr())
+    _check(load_library().metasd_rope_append(C.byref(rope.c), C.byref(pages), _DTYPES.get(lead.dtype, -1), rows, H, qp, ldq, op, ldo, kp, ldk, vp, ldv, pos.data_ptr(), sp, st))
     return out
 
 
@@ -616,12 +619,14 @@ def attn_pages(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, start: 
     B, width = table.shape
     if start.numel() != B + 1 or lens.numel() != B or pool.get_device() != q.get_device():
         raise ValueError("attn_pages: start has batch + 1 entries, lens batch, the pool is on the same device")
+    ldo = H * hd
     if out is None:
         out = torch.empty((rows, H, hd), dtype=q.dtype, device=q.device)
+    elif rows:
+        ldo = _rows3("out", out, rows, H, hd, q)
     if rows == 0:
         return out
-    dt = _DTYPES.get(q.dtype, -1)
-    ldq, ldo = _rows3("q", q, rows, H, hd, q), _rows3("out", out, rows, H, hd, q)
+    dt, ldq = _DTYPES.get(q.dtype, -1), _rows3("q", q, rows, H, hd, q)
     pages = _pages(pool, page, n_kv_heads, hd)
     n = _attn_scratch(B, H, n_kv_heads, hd, dt, max_new, max_len, q.get_device())
     scratch = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None

@@ -6,7 +6,6 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
-#include <cstring>
 
 #include "accept_probs.h"
 #include "pages.h"
@@ -70,6 +69,9 @@ void rope_table(const metasd_rope& r, RopeTab* t) {
     t->rot = r.rot_dim;
     t->blocks = r.rot_dim % (r.style == METASD_ROPE_HALF ? 16 : 8) == 0;
     t->gain = r.gain;
+    // theta^(-2 i / n) as the product of the powers at the bits of i: six calls instead of 64
+    double bit[6];
+    for (int k = 0; k < 6; ++k) bit[k] = 2 << k < n ? std::pow(theta, -(double)(2 << k) / n) : 1.0;
     double a = 0, b = 0;
     if (r.scaling == METASD_ROPE_INDEX) {
         auto place = [&](double turns) { return n * std::log(r.orig_ctx / (turns * TWO_PI)) / (2.0 * std::log(theta)); };
@@ -77,7 +79,8 @@ void rope_table(const metasd_rope& r, RopeTab* t) {
         b = std::min(n - 1, std::ceil(place(r.low)));
     }
     for (int i = 0; i < r.rot_dim / 2; ++i) {
-        double f = std::pow(theta, -2.0 * i / n);
+        double f = 1.0;
+        for (int k = 0; k < 6; ++k) if (i >> k & 1) f *= bit[k];
         if (r.scaling == METASD_ROPE_LINEAR) f /= r.factor;
         else if (r.scaling == METASD_ROPE_WAVE) {
             const double turns = r.orig_ctx * f / TWO_PI, keep = std::min(1.0, std::max(0.0, (turns - r.low) / ((double)r.high - r.low)));
@@ -221,10 +224,8 @@ int32_t metasd_rope_append(const metasd_rope* rope, const metasd_pages* pages, i
     if (k) { check_rows("k", k, k_ld, (int64_t)pages->n_kv_heads * hd, es, &bad); check_rows("v", v, v_ld, (int64_t)pages->n_kv_heads * hd, es, &bad); }
     if (q == q_out && q && q_ld != q_out_ld) bad = "q_out";
     if (bad) return fail_global(METASD_E_INVALID, "rope_append: rows of %s must start on 16 bytes and not overlap", bad);
-    // the table of the last description is kept per thread: its powers cost more than the launch
-    thread_local metasd_rope have{};
-    thread_local RopeTab tab{};
-    if (memcmp(&have, rope, sizeof have)) { rope_table(*rope, &tab); have = *rope; }
+    RopeTab tab{};
+    rope_table(*rope, &tab);
     const int n_cu = n_cu_of_device();
     if (!n_cu) return fail_global(METASD_E_HIP, "rope_append: cannot query the device");
     const Pool pl = pool_of(*pages);
@@ -268,7 +269,7 @@ int32_t metasd_attn_pages_scratch(int32_t batch, int32_t n_heads, int32_t n_kv_h
     if (dtype != METASD_F32 && dtype != METASD_BF16) return fail_global(METASD_E_INVALID, "attn_pages_scratch: dtype");
     const int n_cu = n_cu_of_device();
     if (!n_cu) return fail_global(METASD_E_HIP, "attn_pages_scratch: cannot query the device");
-    const PagesPlan p = plan_pages(batch, n_kv_heads, n_heads / n_kv_heads, head_dim, max_new, max_len, dtype == METASD_BF16 ? 1 : 2, n_cu);
+    const PagesPlan p = plan_pages(batch, n_kv_heads, n_heads / n_kv_heads, head_dim, max_new, max_len, dtype == METASD_BF16 ? 1 : 3, n_cu);
     *bytes_out = pages_records(p, batch, n_kv_heads, head_dim) * sizeof(float);
     return METASD_OK;
 }
@@ -292,7 +293,7 @@ int32_t metasd_attn_pages(const metasd_pages* pages, int32_t dtype, int32_t rows
     if (bad) return fail_global(METASD_E_INVALID, "attn_pages: rows of %s must start on 16 bytes and not overlap", bad);
     const int n_cu = n_cu_of_device();
     if (!n_cu) return fail_global(METASD_E_HIP, "attn_pages: cannot query the device");
-    const PagesPlan p = plan_pages(batch, KH, n_heads / KH, hd, max_new, max_len, dtype == METASD_BF16 ? 1 : 2, n_cu);
+    const PagesPlan p = plan_pages(batch, KH, n_heads / KH, hd, max_new, max_len, dtype == METASD_BF16 ? 1 : 3, n_cu);
     const size_t need = pages_records(p, batch, KH, hd) * sizeof(float);
     if (need && (!scratch || !aligned(scratch) || scratch_bytes < need)) return fail_global(METASD_E_WORKSPACE, "attn_pages: scratch of %zu bytes, 16-byte aligned, needed (metasd_attn_pages_scratch)", need);
     const PagesAttn a{q, out, (size_t)q_ld, (size_t)out_ld, 0, table, start, lens, (float*)scratch, scale * 1.44269504088896341f, 0, batch, width, rows, n_heads, n_heads / KH,

@@ -31,7 +31,8 @@ __device__ __forceinline__ int pages_seen(const PagesReq& r, int G, int c0, int 
     const int last = (min(c0 + cols, r.n * G) - 1) / G;
     return max(min(r.L, r.L - r.n + last + 1), 0);
 }
-__device__ __forceinline__ int pages_records_of(const PagesAttn& a, int seen) { return max(1, min(((seen + 31) / 32 + a.spw - 1) / a.spw, a.nsp)); }
+__device__ __forceinline__ int sub_blocks(int seen) { return (int)(((unsigned)seen + 31) / 32); }
+__device__ __forceinline__ int pages_records_of(const PagesAttn& a, int seen) { return max(1, min((sub_blocks(seen) + a.spw - 1) / a.spw, a.nsp)); }
 
 // Byte i of w as the scale of a conversion, which goes by the exponent of its operand alone: the bits of the other bytes that this leaves in sign
 // and mantissa do not matter (one instruction instead of two; a layout test and the tests of the values would notice).
@@ -112,7 +113,7 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
     const PagesReq rq = pages_req(a, b, pl.shift);
     const int ncol = rq.n * a.G, c0 = cg * W * CT, group = col / W;      // group: which terms of a row this lane's column carries
     if (c0 >= ncol) return;                            // workgroup-uniform, as is the next
-    const int seen = pages_seen(rq, a.G, c0, W * CT), nsub = (seen + 31) / 32, nrec = pages_records_of(a, seen);
+    const int seen = pages_seen(rq, a.G, c0, W * CT), nsub = sub_blocks(seen), nrec = pages_records_of(a, seen);
     if (sp >= nrec) return;
     const int s1 = sp == nrec - 1 ? nsub : min(nsub, (sp + 1) * a.spw);
     const int all_see = rq.L - rq.n + c0 / a.G;        // every column sees the positions up to here
@@ -414,7 +415,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 4 : 3) void attn_pages_long_kerne
     const PagesReq rq = pages_req(a, b, pl.shift);
     const int ncol = rq.n * a.G;
     if (cg * GC >= ncol) return;
-    const int seen = pages_seen(rq, a.G, cg * GC, GC), nsub = (seen + 31) / 32, nrec = pages_records_of(a, seen);
+    const int seen = pages_seen(rq, a.G, cg * GC, GC), nsub = sub_blocks(seen), nrec = pages_records_of(a, seen);
     if (sp >= nrec) return;
     const int it0 = sp * a.spw / 2, it1 = ((sp == nrec - 1 ? nsub : min(nsub, (sp + 1) * a.spw)) + 1) / 2;      // steps of 64 positions
     const int c0 = cg * GC + wave * 16;

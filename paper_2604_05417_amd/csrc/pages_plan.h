@@ -36,7 +36,7 @@ inline PagesPlan plan_pages(int B, int KH, int G, int hd, int max_new, int max_l
     p.pack = terms == 1 || cols > 8 ? 1 : cols > 4 ? 2 : 4;
     p.cols = 16 * p.ct / p.pack;
     p.ncg = (int)((cols + p.cols - 1) / p.cols);
-    const int nsub = std::max(1, (max_len + 31) / 32);
+    const int nsub = (std::max(1, max_len) - 1) / 32 + 1;
     p.wide = cols >= PAGES_WIDE;
     if (p.wide) {
         p.ct = 1;

@@ -6,6 +6,7 @@ import subprocess
 
 import numpy as np
 import pytest
+import torch
 
 import pages_ref as R
 import paper_2604_05417_amd as M
@@ -104,6 +105,82 @@ def test_accept_refusals(lib, kw, text):
     a = dict(P=OK, p_row=400, p_pos=100, Q=OK, q_row=300, q_pos=100, d=OK, n=OK, u=OK, w=OK, rows=2, gamma=3, V=100)
     a.update(kw)
     refused(lib, lib.metasd_accept_probs(a["P"], a["p_row"], a["p_pos"], a["Q"], a["q_row"], a["q_pos"], a["d"], a["n"], a["u"], a["w"], a["rows"], a["gamma"], a["V"], OK, OK, None), text)
+
+
+def test_wrappers_refuse_what_is_missing():
+    q, i = torch.zeros(2, 4, 64), torch.zeros(2, dtype=torch.int32)
+    pool = torch.zeros(4, M.page_bytes(2, 64, 16), dtype=torch.uint8)
+    for args in ((None, None, None, i, i, pool), (None, q, None, i, i, pool), (q, q, q, i, None, pool), (q, q, q, i, i, None)):
+        with pytest.raises(ValueError, match="k with v, slots and pool"):
+            M.rope_append(*args, 16, 2, 64, M.Rope())
+    for call in (lambda: M.rope_append(q, None, None, i, None, None, 16, 2, 64, M.Rope()), lambda: M.kv_rows(pool, i, 16, 2, 64),
+                 lambda: M.attn_pages(q, pool, i.reshape(2, 1), i, i, 16, 2, 0.1, 1, 16), lambda: M.page_plan(i.reshape(2, 1), i, i, i, i, i, 16, 2),
+                 lambda: M.accept_probs(torch.zeros(2, 2, 8), None, i.reshape(2, 1), None, torch.zeros(2, 1), torch.zeros(2))):
+        with pytest.raises(ValueError, match="no CPU fallback"):
+            call()
+
+
+PLAN_SRC = '''#include "pages_plan.h"
+extern "C" void plan(int B, int KH, int G, int hd, int max_new, int max_len, int terms, int n_cu, size_t limit, long* o) {
+    const msd::PagesPlan p = msd::plan_pages(B, KH, G, hd, max_new, max_len, terms, n_cu, limit);
+    const long x[] = {p.wide, p.ct, p.pack, p.cols, p.nw, p.ncg, p.spw, p.nsp, (long)msd::pages_records(p, B, KH, hd)};
+    for (int i = 0; i < 9; ++i) o[i] = x[i];
+}'''
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    d = tmp_path_factory.mktemp("pages_plan")
+    (d / "p.cpp").write_text(PLAN_SRC)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2604_05417_amd", "csrc"), "-o", str(d / "p.so"), str(d / "p.cpp")], check=True)
+    f = C.CDLL(str(d / "p.so")).plan
+    f.argtypes = [C.c_int] * 8 + [C.c_size_t, C.POINTER(C.c_long)]
+
+    def call(*a, n_cu=256, limit=2 ** 63):
+        o = (C.c_long * 9)()
+        f(*a, n_cu, limit, o)
+        return dict(zip(("wide", "ct", "pack", "cols", "nw", "ncg", "spw", "nsp", "records"), o))
+    return call
+
+
+@pytest.mark.parametrize("terms", [1, 3])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("B,KH,G", [(1, 1, 1), (1, 32, 1), (24, 8, 4), (3, 2, 8), (1, 1, 256), (4096, 8, 1), (4096, 1024, 1), (65535, 64, 1)])
+def test_attention_plan(plan, B, KH, G, hd, terms):
+    """Every column and every position has its workgroup, a launch holds the grid, and records stay within the room that there is."""
+    for max_new in (1, 2, 3, 7, 16, 17, 200, 1000, 1 << 20):
+        if B * KH * G * max_new > 1 << 26:
+            continue
+        for max_len in (1, 31, 33, 500, 513, 4000, 100001, 2 ** 31 - 1):
+            for n_cu in (256, 64, 1):
+                p = plan(B, KH, G, hd, max_new, max_len, terms, n_cu=n_cu)
+                nsub = max(1, (max_len + 31) // 32)
+                assert p["cols"] == (64 if p["wide"] else 16 * p["ct"] // p["pack"]) and p["ncg"] * p["cols"] >= max_new * G > (p["ncg"] - 1) * p["cols"]
+                assert p["nsp"] * p["spw"] >= nsub > (p["nsp"] - 1) * p["spw"] and p["spw"] % (2 if p["wide"] else p["nw"]) == 0
+                assert p["pack"] == 1 or (terms == 3 and max_new * G <= 16 // p["pack"])
+                assert p["nw"] == 4 or p["nsp"] == 1
+                units = -(-B * KH // 8) * 8 if p["wide"] else B * KH
+                assert units * p["ncg"] * p["nsp"] * 64 * p["nw"] < 1 << 32
+                assert p["records"] == (0 if p["nsp"] == 1 else B * KH * p["ncg"] * p["nsp"] * p["cols"] * (hd + 4))
+                for limit in (0, p["records"] // 2, p["records"]):
+                    r = plan(B, KH, G, hd, max_new, max_len, terms, n_cu=n_cu, limit=limit)
+                    assert r["records"] <= limit and r["nsp"] * r["spw"] >= nsub
+                    assert limit < p["records"] or r == p
+
+
+@pytest.mark.parametrize("ncg,nsp", [(5, 1), (24, 1), (63, 1), (24, 3), (7, 16), (600, 1)])
+def test_order_of_long_blocks(ncg, nsp):
+    """The order that attn_pages_long_kernel gives its workgroups, written out: every (pair, column group, span) once."""
+    for units in (1, 2, 4, 5, 40, 130):
+        per, seen = ncg * nsp, set()
+        most = min(units, (511 + per) // per)
+        for y in range(units * per):
+            bundle = y // (most * per)
+            n_units, z = min(most, units - bundle * most), y - bundle * most * per
+            rnd = z >> 5
+            place = min(32 * rnd + 31, n_units * per - 1) - (z & 31) if rnd & 1 else z
+            seen.add((bundle * most + place // nsp % n_units, ncg - 1 - place // (nsp * n_units), place % nsp))
+        assert seen == {(u, c, s) for u in range(units) for c in range(ncg) for s in range(nsp)}
 
 
 def test_reference_quantiser():
