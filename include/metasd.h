@@ -396,7 +396,8 @@ int32_t metasd_page_plan(int32_t* table, int32_t batch, int32_t width, int32_t* 
  *   WAVE    by the turns t = orig_ctx f_i / (2 pi) that a pair makes in the original context: s = clamp((t - low) / (high - low), 0, 1),
  *           f_i (s + (1 - s) / factor)
  *   INDEX   by the place of the pair: with i(t) = rot_dim ln(orig_ctx / (2 pi t)) / (2 ln theta), a = max(floor(i(high)), 0) and
- *           b = min(ceil(i(low)), rot_dim - 1), s = clamp((i - a) / max(b - a, 0.001), 0, 1), f_i ((1 - s) + s / factor) */
+ *           b = min(ceil(i(low)), rot_dim - 1), s = clamp((i - a) / max(b - a, 0.001), 0, 1), f_i ((1 - s) + s / factor)
+ * theta > 1, factor >= 2^-16, gain not 0, orig_ctx >= 1, 0 < low < high. */
 #define METASD_ROPE_HALF 0
 #define METASD_ROPE_PAIRS 1
 #define METASD_ROPE_PLAIN 0

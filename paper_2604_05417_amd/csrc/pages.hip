@@ -56,7 +56,7 @@ const char* check_rope(const metasd_rope& r, int hd) {
     if (!(r.theta > 1.f) || !std::isfinite(r.theta)) return "theta must be above 1";
     if (!std::isfinite(r.gain) || r.gain == 0.f) return "gain";
     if (r.scaling < METASD_ROPE_PLAIN || r.scaling > METASD_ROPE_INDEX) return "scaling";
-    if (r.scaling != METASD_ROPE_PLAIN && (!(r.factor > 0.f) || !std::isfinite(r.factor))) return "factor must be positive";
+    if (r.scaling != METASD_ROPE_PLAIN && (!(r.factor >= 0x1p-16f) || !std::isfinite(r.factor))) return "factor must be at least 2^-16";       // angles stay below 2^47
     if (r.scaling >= METASD_ROPE_WAVE && (r.orig_ctx < 1 || !(r.low > 0.f) || !(r.high > r.low) || !std::isfinite(r.high))) return "orig_ctx >= 1 and 0 < low < high";
     return nullptr;
 }

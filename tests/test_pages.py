@@ -88,6 +88,14 @@ def test_rope_refusals(lib, kw, text):
         refused(lib, lib.metasd_rope_append(C.byref(r.c), C.byref(pages()), 0, 4, 2, OK, 128, OK, 128, OK, 128, OK, 128, OK, OK, None), field)
 
 
+@pytest.mark.parametrize("scaling", ["linear", "wave", "index"])
+def test_rope_refuses_angles_beyond_its_reduction(lib, scaling):
+    """Positions times frequencies over a tiny factor would leave the range that the sines are reduced from."""
+    for factor in (2.0 ** -17, 1e-30, -1.0, math.nan, math.inf):
+        r = M.Rope("half", 64, scaling=scaling, factor=factor)
+        refused(lib, lib.metasd_rope_append(C.byref(r.c), C.byref(pages()), 0, 4, 2, OK, 128, OK, 128, OK, 128, OK, 128, OK, OK, None), "factor")
+
+
 @pytest.mark.parametrize("kw,text", [(dict(q=None), "NULL"), (dict(lens=None), "NULL"), (dict(dtype=3), "dtype"), (dict(rows=0), "rows"), (dict(H=3), "n_heads"), (dict(batch=0), "batch"),
                                      (dict(batch=65536), "batch"), (dict(width=0), "width"), (dict(width=1 << 28), "31 bits"), (dict(max_new=0), "max_new"), (dict(max_len=0), "max_len"),
                                      (dict(scale=0.0), "scale"), (dict(scale=math.nan), "scale"), (dict(q_ld=129), "rows of q"), (dict(out=OK + 4), "rows of out"), (dict(out=OK), "which is q"),
