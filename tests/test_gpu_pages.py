@@ -327,6 +327,28 @@ def test_attention_of_prompts(dt, H, KH, hd, page):
     check_attn(q, pool, table, K, V, lens, n_new, page, KH, 1 / math.sqrt(hd))
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,KH,hd,L,n", [(2, 1, 128, 2000, 300), (1, 1, 64, 4100, 257), (4, 2, 32, 900, 700)])
+def test_attention_of_prompts_behind_long_contexts(dt, H, KH, hd, L, n):
+    """Long blocks whose positions are split over workgroups and merged."""
+    rng = np.random.default_rng(L)
+    pool, table, K, V = filled(rng, [L], KH, hd, 64)
+    q = torch.randn((n, H, hd), generator=torch.Generator().manual_seed(7)).to(dt).to(DEV)
+    for hint in (L, 50, 3 * L):
+        check_attn(q, pool, table, K, V, [L], [n], 64, KH, 1 / math.sqrt(hd), max_len=hint)
+
+
+@pytest.mark.parametrize("dt,B,H,KH,n", [(torch.bfloat16, 6, 16, 16, 500), (torch.float32, 3, 16, 16, 300), (torch.bfloat16, 1120, 256, 1, 1), (torch.float32, 700, 256, 1, 1)])
+def test_attention_of_many_long_blocks(dt, B, H, KH, n):
+    """More workgroups than CUs, in several rounds and bundles."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(1, 60, B) + (n if n > 1 else 0)
+    n_new = [int(rng.integers(max(1, n - 100), n + 1)) for _ in range(B)]
+    pool, table, K, V = filled(rng, lens, KH, 32, 16)
+    q = torch.randn((sum(n_new), H, 32), generator=torch.Generator().manual_seed(8)).to(dt).to(DEV)
+    check_attn(q, pool, table, K, V, lens, n_new, 16, KH, 0.2, max_new=n)
+
+
 def test_attention_with_large_scores_and_marked_positions():
     """Scores of hundreds (the weight is on one position); a marked position makes the rows that see it NaN and no others."""
     rng = np.random.default_rng(8)
