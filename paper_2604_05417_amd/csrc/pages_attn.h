@@ -8,7 +8,7 @@
 namespace msd {
 
 struct PagesAttn {
-    const void* q;           // [rows][H][hd], rows ldq elements apart: bf16 (one term) or fp32 (two)
+    const void* q;           // [rows][H][hd], rows ldq elements apart: bf16 (one term) or fp32 (three)
     void* out;               // the same, ldo apart; split != 0: two bf16 terms (store_terms4, lo_off)
     size_t ldq, ldo, lo_off;
     const int *table, *start, *lens;
@@ -85,9 +85,14 @@ __device__ __forceinline__ void pages_store4(const PagesAttn& a, int row, int h,
 //   S^T[pos][col] = K . q^T    A = K codes straight from the page, widened to bf16 (exact: 2 significant bits times a power of two)
 //   O^T[d][col]  += V^T . P^T  A = V widened and transposed pairwise in registers, B = P straight from the registers that held S^T (slot 8 g
 //                              + i of the 32 positions stands for 4 g + i or 16 + 4 g + i - 4)
-// TERMS = 2: q and P as two bf16 terms each.  The maximum is only raised, and O rescaled, when a score exceeds it by more than 2^8; sums are in
-// 32 bits.  The next sub-block is requested while the present one is multiplied.  The wavefronts merge through LDS; a context of one
-// record is written as it is, several are merged by pages_merge_kernel.
+// TERMS = 3 (fp32 rows): q and P as three bf16 terms each, 24 bits; with PACK 2 or 4 the terms of a pair lie in different columns of one
+// product.  The maximum is only raised, and O rescaled, when a score exceeds it by more than 2^8; sums are in 32 bits.  The next sub-block is
+// requested while the present one is multiplied.  The wavefronts merge through LDS; a context of one record is written as it is, several are
+// merged by pages_merge_kernel.
+// What bounds it: HBM for many long contexts - 32 requests of 8 rows behind 4104 positions, 32 heads of 128, fp32 rows: 578 MB in 118 us, 4.9 TB/s (min
+// 106), where the same requests without any arithmetic take 100 - with 324 vector instructions per 32 positions, two thirds of the cycles,
+// and the matrix unit a quarter.  One request of 6 rows behind 2053: 8.5 us and the merge's 3.9, a chain of q, page number, tile and
+// products per wavefront.  A deeper prefetch, non-temporal loads and eight or sixteen spans per CU change nothing.
 template <int HD, int CT, int TERMS, int PACK, int NW>
 struct PagesForm {
     static constexpr int W = 16 / PACK;                               // (row, head) pairs of a column tile
@@ -581,7 +586,8 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 4 : 3) void attn_pages_long_kerne
     if (rec && g == 0) *reinterpret_cast<float2*>(rec + HD) = make_float2(mx, sum);
 }
 
-// Records of a column merged in their order.  HD / 4 lanes per (request, row, head).   grid ceil(B max_new H / units), block 256
+// Records of a column merged in their order.  HD / 4 lanes per (request, row, head).  Bound by its launch and one round of requests: 3.9 us for 192
+// columns of 6 records.   grid ceil(B max_new H / units), block 256
 template <int HD, int TERMS>
 __global__ __launch_bounds__(256) void pages_merge_kernel(PagesAttn a, Pool pl, int cols) {
     constexpr int LN = HD / 4, OS = HD + 4;

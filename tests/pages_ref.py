@@ -4,7 +4,7 @@ import math
 import numpy as np
 
 GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
-H24, H8, H16 = 2.0 ** -24, 2.0 ** -8, 2.0 ** -16        # half a step of fp32 and bf16 relative to a value; of two bf16 terms
+H24, H8 = 2.0 ** -24, 2.0 ** -8        # half a step of fp32 and bf16 relative to a value
 
 
 def scale_exponent(amax):
@@ -122,9 +122,9 @@ def page_plan(table, held, ring, state, lens, n_new, page, rows):
 def attention(q, K, V, lens, n_new, scale, bf16):
     """q [rows, H, hd], K, V lists of [L, KH, hd] per request (held values).  Returns (out, bound).
 
-    Bound.  A score is off by A = scale sum |q| |k| times: fp32, the two-term q (2^-16); its sum in 32 bits (hd + 4 terms of 2^-24, each
+    Bound.  A score is off by A = scale sum |q| |k| times: fp32, the three-term q (2^-24); its sum in 32 bits (hd + 4 terms of 2^-24, each
     product exact).  The exponent's argument and exp2 add (|score| + 4) 2^-23.  An error d of all scores moves every weight by at most a
-    factor e^(2 d), 2.1 d while d is small.  Weights: bf16, half a step 2^-8 (fp32: 2^-16); their sum and the products' L 2^-24; the merges
+    factor e^(2 d), 2.1 d while d is small.  Weights: bf16, half a step 2^-8 (fp32, three terms: 2^-24); their sum and the products' L 2^-24; the merges
     and the division 64 2^-24.  Output in bf16: half a step of it."""
     rows, H, hd = q.shape
     out, bound = np.zeros((rows, H, hd)), np.zeros((rows, H, hd))
@@ -143,8 +143,8 @@ def attention(q, K, V, lens, n_new, scale, bf16):
                     w = np.exp(s - s.max())
                     w /= w.sum()
                     out[at + i, h] = w @ v
-                    d = float((scale * (np.abs(k) @ np.abs(x))).max()) * ((0 if bf16 else H16) + (hd + 4) * H24) + (np.abs(s).max() * 1.5 + 4) * 2 * H24
-                    rel = 2.1 * d + (H8 if bf16 else H16) + (see + 64) * H24
+                    d = float((scale * (np.abs(k) @ np.abs(x))).max()) * ((0 if bf16 else H24) + (hd + 4) * H24) + (np.abs(s).max() * 1.5 + 4) * 2 * H24
+                    rel = 2.1 * d + (H8 if bf16 else H24) + (see + 64) * H24
                     bound[at + i, h] = (w @ np.abs(v)) * rel * 1.01 + (H8 * np.abs(out[at + i, h]) * 1.01 if bf16 else 0) + 1e-37
         at += n
     return out, bound
