@@ -169,7 +169,7 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
     }
     Words<KC> kd[2], vd[2], vs[2];
     uint32_t ks[2];
-    const int tshift = pl.shift - 4, tlast = max(seen - 1, 0) >> 4;
+    const int tshift = pl.shift - 4, tlast = min(max(seen - 1, 0) >> 4, 2 * s1 - 1);
     const int* tab = a.table + (size_t)b * a.width;
     const int first = sp * a.spw + wave;               // this wavefront's sub-blocks: first, first + NW, ..
     // page numbers of the next 32 sub-blocks, two tiles each, one a lane: a request finds them in a register
@@ -210,8 +210,7 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
     }
     for (int s = first, k = 0; s < s1; s += NW, ++k) {
         const int p0 = s * 32;
-        const bool more = s + NW < s1;
-        if (more && ((k + 1) & 31) == 0) look_up(k + 1);
+        if (((k + 1) & 31) == 0) look_up(k + 1);
         // ---- scores
         __builtin_amdgcn_s_setprio(1);
         f32x4 sc[CT][2];
@@ -245,7 +244,7 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
                     sc[0][t][v] += rotated<8>(sc[0][t][v]);
                     if constexpr (PACK == 4) sc[0][t][v] += rotated<4>(sc[0][t][v]);
                 }
-        if (more) request_k(k + 1);
+        request_k(k + 1);                              // also behind the last: what is requested on one of two paths is waited for on both
         if (p0 + 31 > all_see) {                       // some column does not see all 32 positions
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -345,7 +344,7 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
                 }
         }
         __builtin_amdgcn_s_setprio(0);
-        if (more) request_v();
+        request_v();
     }
     // ---- merge the wavefronts
     if constexpr (F::QL) __syncthreads();              // q has been read
