@@ -37,8 +37,8 @@ __device__ __forceinline__ unsigned char* tile_at(const Pool& pl, int page, int 
 // most PLAN_BATCH of them, 20 bytes each, from L2), so that nothing has to be handed from one to another; the pages that change hands are
 // dealt out over all of them.  Pages are taken from the front of the ring and given back behind its last, two stretches that do not meet
 // because the ring has room for every page there is.  The counts of the state and of the requests are read by all and written by the
-// workgroup that comes to its end last.  Bound by the chain of requests, three sums and their barriers, a search and a page number: 4.0 us for 32
-// requests and 256 rows, 8.4 for 300 and 123 000 (4 MB, under 1 us of HBM).
+// workgroup that comes to its end last.  Bound by the chain of requests, three sums and their barriers, a search and a page number: 4.2 us for 32
+// requests and 256 rows, 8.5 for 300 and 126 000 (1.2 MB, under 1 us of HBM).
 constexpr int PLAN_BATCH = 4096, PLAN_PER = 4;      // requests of a call, and of a thread
 
 struct PlanArgs {

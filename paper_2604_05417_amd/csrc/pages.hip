@@ -200,9 +200,8 @@ int32_t metasd_page_plan(int32_t* table, int32_t batch, int32_t width, int32_t* 
     const PlanArgs a{table, held, ring, state, lens, n_new, slots, pos, start, served, batch, width, n_pages, shift_of(page), rows};
     hipStream_t st = (hipStream_t)hip_stream;
 #define GO(NT) hipLaunchKernelGGL((page_plan_kernel<NT>), dim3(std::max(1, (rows + NT - 1) / NT)), dim3(NT), 0, st, a)
-    // A call of few requests and few rows is bound by its barriers: four wavefronts meet sooner than
-    // sixteen (64 requests, 256 rows: 4.2 us against 5.6). Sixteen repeat the scan over the requests
-    // for fewer groups of rows (122 000 rows: 8.5 us against 11.4 with four).
+    // A call of few requests and few rows is bound by its barriers: four wavefronts meet sooner than sixteen (32 requests, 256 rows: 4.2 us against
+    // 5.6).  Sixteen repeat the scan over the requests for fewer groups of rows (126 000 rows: 8.5 us against 11.4 with four).
     if (batch <= 256 * PLAN_PER && rows <= 1024) GO(256); else GO(1024);
 #undef GO
     if (hipGetLastError() != hipSuccess) return fail_global(METASD_E_HIP, "page_plan: launch failed");

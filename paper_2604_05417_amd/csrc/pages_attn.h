@@ -89,9 +89,9 @@ __device__ __forceinline__ void pages_store4(const PagesAttn& a, int row, int h,
 // product.  The maximum is only raised, and O rescaled, when a score exceeds it by more than 2^8; sums are in 32 bits.  The next sub-block is
 // requested while the present one is multiplied.  The wavefronts merge through LDS; a context of one record is written as it is, several are
 // merged by pages_merge_kernel.
-// What bounds it: HBM for many long contexts - 32 requests of 8 rows behind 4104 positions, 32 heads of 128, fp32 rows: 578 MB in 118 us, 4.9 TB/s (min
-// 106), where the same requests without any arithmetic take 100 - with 324 vector instructions per 32 positions, two thirds of the cycles,
-// and the matrix unit a quarter.  One request of 6 rows behind 2053: 8.5 us and the merge's 3.9, a chain of q, page number, tile and
+// What bounds it: HBM for many long contexts - 32 requests of 8 rows behind 4104 positions, 32 heads of 128, fp32 rows: 578 MB in 104 - 119 us, 4.9 - 5.5 TB/s,
+// where the same requests without any arithmetic take 100 and bf16 rows 102 - with 305 vector instructions per 32 positions, two thirds of the
+// cycles, and the matrix unit a quarter.  One request of 6 rows behind 2053: 7.8 us and the merge's 4, a chain of q, page number, tile and
 // products per wavefront.  A deeper prefetch, non-temporal loads and eight or sixteen spans per CU change nothing.
 template <int HD, int CT, int TERMS, int PACK, int NW>
 struct PagesForm {
