@@ -15,6 +15,7 @@ bounded sample of the same workload on this host.
 from __future__ import annotations
 
 import argparse
+import gc
 import json
 import os
 import sys
@@ -135,6 +136,7 @@ def main():
 
     for _ in range(Wm):
         one_round()
+    gc.collect()                                  # or the collection of what the imports left (40 ms) falls into the timed steps, by chance
     torch.cuda.synchronize()
     # ---- timed region: exactly K steps
     t1 = time.perf_counter()
@@ -286,6 +288,7 @@ def bench_c5(args):
 
     for _ in range(Wm):
         one_round()
+    gc.collect()
     torch.cuda.synchronize()
     t1 = time.perf_counter()
     toks, accs = 0, []
@@ -372,6 +375,7 @@ def bench_c3(args):
 
     for _ in range(Wm):
         one_round()
+    gc.collect()
     torch.cuda.synchronize()
     t1 = time.perf_counter()
     toks, accs, arms = 0, [], []
@@ -476,6 +480,7 @@ def bench_c4_tree(args):
     for name, use_tree in (("chain", False), ("tree", True)):
         for _ in range(Wm):
             one_round(use_tree)
+        gc.collect()
         torch.cuda.synchronize()
         t1 = time.perf_counter()
         accs = [one_round(use_tree) for _ in range(K_steps)]
@@ -574,6 +579,7 @@ def bench_c4_heads(args):
     for name, use_tree in (("chain", False), ("tree", True)):
         for _ in range(Wm):
             one_round(use_tree)
+        gc.collect()
         torch.cuda.synchronize()
         t1 = time.perf_counter()
         accs = [one_round(use_tree) for _ in range(K_steps)]
@@ -634,6 +640,7 @@ def bench_c4_policies(args):
             g.swap_weight(k, head_index, heads[k][0])
         g.set_context(cfg["prompt"], kv_prefilled=True)
         seg, new_tokens, accs, arms = 0, 0, [], [0] * K
+        gc.collect()
         torch.cuda.synchronize()
         t1 = time.perf_counter()
         for _ in range(rounds):
