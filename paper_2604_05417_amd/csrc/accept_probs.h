@@ -62,10 +62,11 @@ __device__ __forceinline__ double span_sum(const float* p, const float* q, int v
 
 // One workgroup per request.  The tests are exact: u q and p are products and numbers of 24 bits, compared in 64.  Then one row of P - and,
 // behind a rejection, one of Q - is all that is read, once: wavefront i sums the weights of its span of the vocabulary (256 tokens at a time,
-// both in their ascending order), and the one whose span the drawn sum falls into reads that again, from L2, to find the token.
-// What bounds it: for one request the chain n - d - p, q - row - sums - token (6 - 8 us at 32000 tokens), for hundreds HBM: 511 requests of 6
-// drafts at 32000 tokens, 103 MB in 24.8 us, 4.2 TB/s.
-//  grid (requests), block AP_NT
+// both in their ascending order), and all of them read the span that the drawn sum falls into again, from L2, to find the token (the
+// span's wavefront alone, 256 tokens after the other: 32 requests 11.0 us instead of 9.0, of 128 256 tokens 28 instead of 17.4).
+// What bounds it: up to hundreds of requests the chain n - d - p, q - row - sums - token, 8.0 us for one at 32000 tokens (no faster with twice the
+// requests in flight); for hundreds HBM: 511 of 6 drafts at 32000 tokens, 103 MB in 22.7 us, 4.5 TB/s.
+// grid (requests), block AP_NT
 __global__ __launch_bounds__(AP_NT, 8) void accept_probs_kernel(AcceptProbs a) {
     __shared__ int fail, token;
     __shared__ double rest[AP_NW];
@@ -122,37 +123,48 @@ __global__ __launch_bounds__(AP_NT, 8) void accept_probs_kernel(AcceptProbs a) {
         before += x;
     }
     if (mine < 0) mine = last;
-    if (wave == mine) {                                // wavefront-uniform
-        int fallback = -1;
+    if (mine >= 0) {                                   // workgroup-uniform, as is all that decides below
+        // .. read again, 256 tokens a wavefront: the first of them at whose end the sum passes the target has the token
+        const int m0 = mine * span, m1 = min(m0 + span, a.V);
         bool found = false;
-        for (int c = v0; c < v1 && !found; c += 256) {
-            const int v = c + lane * 4;
+        for (int c = m0; c < m1 && !found; c += AP_NW * 256) {
+            const int v = c + (wave * 64 + lane) * 4;
             f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-            if (v < v1) {
+            if (v < m1) {
                 x = law4(p, v, a.V, a.vec);
                 if (q) y = law4(q, v, a.V, a.vec);
             }
             double r[4];
             rest4(x, y, v, out, r);
             const double sum = (r[0] + r[1]) + (r[2] + r[3]), scan = dpp_scan(sum);
-            const unsigned long long some = __ballot(sum > 0.0), pass = __ballot(sum > 0.0 && base + scan > target);
-            // the first token at which the sum passes the target, or the last with a weight so far
-            const int at = pass ? __ffsll(pass) - 1 : some ? 63 - __clzll(some) : -1;
-            if (at >= 0) {
+            __syncthreads();                           // the sums there have been read
+            if (lane == 63) rest[wave] = scan;
+            __syncthreads();
+            int at = -1;
+            last = -1;
+            before = base;
+            for (int i = 0; i < AP_NW; ++i) {
+                const double t = rest[i];
+                if (t > 0.0) last = i;
+                if (at < 0 && t > 0.0 && before + t > target) { at = i; base = before; }
+                before += t;
+            }
+            found = at >= 0;
+            if (wave == (found ? at : last)) {         // wavefront-uniform; should rounding leave none: the last token with a weight so far
+                const unsigned long long some = __ballot(sum > 0.0), pass = __ballot(sum > 0.0 && base + scan > target);
+                const int l = found && pass ? __ffsll(pass) - 1 : 63 - __clzll(some);
                 double run = base + (scan - sum);
                 int pick = -1;
                 bool done = false;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     run += r[e];
-                    if (r[e] > 0.0 && !done) { pick = v + e; done = pass && run > target; }
+                    if (r[e] > 0.0 && !done) { pick = v + e; done = found && run > target; }
                 }
-                fallback = __builtin_amdgcn_readlane(pick, at);
+                if (lane == l) token = pick;
             }
-            found = pass != 0;
-            base += __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(scan), 63), __builtin_amdgcn_readlane(__double2loint(scan), 63));
+            base = before;
         }
-        if (lane == 0) token = fallback;
     }
     __syncthreads();
     if (tid == 0) a.n_acc[b] = k;

@@ -455,6 +455,23 @@ def test_accept_probs_borders():
     check_accept(P, None, d, [0, 0, 1, 1, 2, 2, 0, 0], u, w)
 
 
+@pytest.mark.parametrize("V", [70000, 300001, 1 << 20])
+def test_accept_probs_of_long_laws(V):
+    """Sixteen tokens of one weight at the borders of the wavefronts' spans and pieces: every one of them is drawn, at and just below its border."""
+    span = -(-V // 4096) * 256
+    at = np.unique(np.minimum([0, 255, 256, 4095, 4096, span - 1, span, span + 255, span + 256, span + 4095, span + 4096, 2 * span - 1, 9 * span + 3, 15 * span - 1, V - 2, V - 1], V - 1))
+    P = np.zeros((32, 2, V), np.float32)
+    P[:, :, at] = 1 / 16
+    w = np.arange(32, dtype=np.float32) // 2 / 16
+    w[1::2] = np.nextafter(w[1::2], np.float32(0))
+    w[1] = 0
+    Q = np.zeros((32, 1, V), np.float32)
+    Q[:, 0, at[::2]] = 1 / 16                                             # behind a rejection: every second of them
+    check_accept(P, Q, np.full((32, 1), at[3]), None, np.zeros((32, 1), np.float32), w)
+    check_accept(P, Q, np.full((32, 1), at[0]), None, np.ones((32, 1), np.float32), w)
+    check_accept(P, None, np.full((32, 1), at[-1]), None, np.ones((32, 1), np.float32), w)
+
+
 def test_accept_probs_strided_and_unaligned():
     rng = np.random.default_rng(3)
     P, Q = laws(rng, 5, 3, 1003)
