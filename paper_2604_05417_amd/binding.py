@@ -503,7 +503,7 @@ def _on(first: torch.Tensor, ints) -> int:
     return _raw_stream(dev)
 
 
-def _rows3(name: str, x: torch.Tensor, rows: int, heads, hd: int, like: torch.Tensor) -> int:
+def _rows3(name: str, x: torch.Tensor, rows: int, heads, hd: int, dtype, dev: int) -> int:
     """Elements between the rows of x: [rows, heads, hd] or [rows, heads * hd], heads next to each other.  heads None: any number of them."""
     shape, stride = x.shape, x.stride()
     if len(shape) == 2:
@@ -512,8 +512,8 @@ def _rows3(name: str, x: torch.Tensor, rows: int, heads, hd: int, like: torch.Te
         wide, ok = shape[1] * hd, shape[2] == hd and stride[2] == 1 and (stride[1] == hd or shape[1] == 1)
     else:
         wide, ok = 0, False
-    if not ok or shape[0] != rows or wide == 0 or (wide % hd if heads is None else wide != heads * hd) or x.dtype is not like.dtype or x.get_device() != like.get_device():
-        raise ValueError(f"{name}: {rows} rows of {'' if heads is None else heads} heads of {hd}, {like.dtype} on {like.device}, heads next to each other; got {tuple(shape)} {x.dtype}")
+    if not ok or shape[0] != rows or wide == 0 or (wide % hd if heads is None else wide != heads * hd) or x.dtype is not dtype or x.get_device() != dev:
+        raise ValueError(f"{name}: {rows} rows of {'' if heads is None else heads} heads of {hd}, {dtype} on cuda:{dev}, heads next to each other; got {tuple(shape)} {x.dtype}")
     return stride[0] if rows > 1 else wide
 
 
@@ -568,29 +568,29 @@ def rope_append(q, k, v, pos: torch.Tensor, slots, pool, page: int, n_kv_heads: 
     if lead is None or (k is not None and (v is None or slots is None or pool is None)):
         raise ValueError("rope_append: q, or k with v, slots and pool, or both")
     st = _on(lead, (pos,) if k is None else (pos, slots))
-    rows = lead.shape[0]
+    rows, dtype, dev = lead.shape[0], lead.dtype, lead.get_device()
     if rows == 0:                                       # nothing to do
         return out if out is not None or q is None else q.new_empty((0, q.shape[1] if q.dim() == 3 else q.shape[1] // head_dim, head_dim))
     if pos.numel() != rows or (k is not None and slots.numel() != rows):
         raise ValueError("rope_append: one position and one slot per row")
     H = ldq = ldo = ldk = ldv = 0
     if q is not None:
-        ldq = _rows3("q", q, rows, None, head_dim, q)
+        ldq = _rows3("q", q, rows, None, head_dim, dtype, dev)
         H = q.numel() // (rows * head_dim)
         if out is None:
             out, ldo = q.new_empty((rows, H, head_dim)), H * head_dim
         else:
-            ldo = _rows3("out", out, rows, H, head_dim, q)
+            ldo = _rows3("out", out, rows, H, head_dim, dtype, dev)
     if k is not None:
-        ldk, ldv = _rows3("k", k, rows, n_kv_heads, head_dim, lead), _rows3("v", v, rows, n_kv_heads, head_dim, lead)
-        if pool.get_device() != lead.get_device():
+        ldk, ldv = _rows3("k", k, rows, n_kv_heads, head_dim, dtype, dev), _rows3("v", v, rows, n_kv_heads, head_dim, dtype, dev)
+        if pool.get_device() != dev:
             raise ValueError(f"pool is on {pool.device}")
         pages = _pages(pool, page, n_kv_heads, head_dim)
     else:
         pages = _Pages(n_kv_heads, head_dim, page, 0, None, 0)
     qp, op = (None, None) if q is None else (q.data_ptr(), out.data_ptr())
     kp, vp, sp = (None, None, None) if k is None else (k.data_ptr(), v.data_ptr(), slots.data_ptr())
-    _check(load_library().metasd_rope_append(C.byref(rope.c), C.byref(pages), _DTYPES.get(lead.dtype, -1), rows, H, qp, ldq, op, ldo, kp, ldk, vp, ldv, pos.data_ptr(), sp, st))
+    _check(load_library().metasd_rope_append(C.byref(rope.c), C.byref(pages), _DTYPES.get(dtype, -1), rows, H, qp, ldq, op, ldo, kp, ldk, vp, ldv, pos.data_ptr(), sp, st))
     return out
 
 
@@ -621,18 +621,19 @@ def attn_pages(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, start: 
     st = _on(q, (table, start, lens))
     rows, H, hd = q.shape
     B, width = table.shape
-    if start.numel() != B + 1 or lens.numel() != B or pool.get_device() != q.get_device():
+    dtype, dev = q.dtype, q.get_device()
+    if start.numel() != B + 1 or lens.numel() != B or pool.get_device() != dev:
         raise ValueError("attn_pages: start has batch + 1 entries, lens batch, the pool is on the same device")
     ldo = H * hd
     if out is None:
         out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((rows, H, hd))
     elif rows:
-        ldo = _rows3("out", out, rows, H, hd, q)
+        ldo = _rows3("out", out, rows, H, hd, dtype, dev)
     if rows == 0:
         return out
-    dt, ldq = _DTYPES.get(q.dtype, -1), _rows3("q", q, rows, H, hd, q)
+    dt, ldq = _DTYPES.get(dtype, -1), _rows3("q", q, rows, H, hd, dtype, dev)
     pages = _pages(pool, page, n_kv_heads, hd)
-    n = _attn_scratch(B, H, n_kv_heads, hd, dt, max_new, max_len, q.get_device())
+    n = _attn_scratch(B, H, n_kv_heads, hd, dt, max_new, max_len, dev)
     scratch = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     _check(load_library().metasd_attn_pages(C.byref(pages), dt, rows, H, q.data_ptr(), ldq, out.data_ptr(), ldo, table.data_ptr(), B, width, start.data_ptr(), lens.data_ptr(),
                                             max_new, max_len, scale, scratch.data_ptr() if n else None, n, st))
@@ -646,8 +647,9 @@ def accept_probs(P: torch.Tensor, Q, d: torch.Tensor, n_draft, u: torch.Tensor, 
     rows, g1, V = P.shape
     if d.shape != (rows, g1 - 1) or u.shape != d.shape or w.shape != (rows,) or (n_draft is not None and n_draft.shape != (rows,)) or (Q is not None and Q.shape != (rows, g1 - 1, V)):
         raise ValueError("accept_probs: P [rows, gamma + 1, V], Q [rows, gamma, V], d and u [rows, gamma], w and n_draft [rows]")
+    dev = P.get_device()
     for t in (P, u, w) if Q is None else (P, Q, u, w):
-        if t.dtype is not torch.float32 or t.get_device() != P.get_device() or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        if t.dtype is not torch.float32 or t.get_device() != dev or (t.stride(-1) != 1 and t.shape[-1] > 1):
             raise ValueError("accept_probs: fp32 on one device, the last dimension contiguous")
     if not (u.is_contiguous() and w.is_contiguous()):
         raise ValueError("accept_probs: u and w contiguous")
