@@ -424,7 +424,7 @@ int32_t metasd_kv_rows(const metasd_pages* pages, const int32_t* slots, int32_t 
  * reads K/V head h / (n_heads / n_kv_heads).  out = softmax(scale q K^T) V, rows behind the last request are left as they were.
  * max_new: the most rows a request has (further ones are not computed), max_len: about the longest context; both only bound the launch,
  * lengths are read on the device.  out is not q; rows <= 2^22.  A table entry outside the pool is read as its last page.  bf16: weights are rounded to bf16 before the
- * product with V; fp32: q and weights are taken as three bf16 terms, 24 bits; sums are in 32 bits.
+ * product with V and divided by the sum of the rounded ones; fp32: q and weights are taken as three bf16 terms, 24 bits; sums are in 32 bits.
  * scratch: metasd_attn_pages_scratch bytes for the same arguments on the same device (may be 0: NULL), used by one call at a time. */
 int32_t metasd_attn_pages_scratch(int32_t batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t max_new,
                                   int32_t max_len, size_t* bytes_out);

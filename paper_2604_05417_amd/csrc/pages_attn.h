@@ -71,6 +71,8 @@ __device__ __forceinline__ Words<N> load_words(const unsigned char* p) {
     return r;
 }
 
+constexpr u32x4 ONES = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};       // bf16
+
 // A row of four outputs.
 template <int TERMS>
 __device__ __forceinline__ void pages_store4(const PagesAttn& a, int row, int h, int hd, int d, const f32x4& y) {
@@ -85,6 +87,8 @@ __device__ __forceinline__ void pages_store4(const PagesAttn& a, int row, int h,
 //   S^T[pos][col] = K . q^T    A = K codes straight from the page, widened to bf16 (exact: 2 significant bits times a power of two)
 //   O^T[d][col]  += V^T . P^T  A = V widened and transposed pairwise in registers, B = P straight from the registers that held S^T (slot 8 g
 //                              + i of the 32 positions stands for 4 g + i or 16 + 4 g + i - 4)
+// TERMS = 1 (bf16 rows): P rounded to bf16, and the sum of a column that of the rounded weights, a product with ones: what a weight is off by
+// cancels where it is the row's only large one, and no lane adds (24 single tokens behind 5000 17.6 / 17.1 us).
 // TERMS = 3 (fp32 rows): q and P as three bf16 terms each, 24 bits; with PACK 2 or 4 the terms of a pair lie in different columns of one
 // product.  The maximum is only raised, and O rescaled, when a score exceeds it by more than 2^8; sums are in 32 bits.  The next sub-block is
 // requested while the present one is multiplied.  The wavefronts merge through LDS; a context of one record is written as it is, several are
@@ -160,10 +164,12 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
     if constexpr (F::QL) __syncthreads();
     f32x4 o[CT][KC][2];
     float mx[CT], sum[CT];
+    f32x4 total[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         mx[ct] = -INFINITY;
         sum[ct] = 0.f;
+        total[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KC; ++j) o[ct][j][0] = o[ct][j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -275,7 +281,7 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
             for (int ct = 0; ct < CT; ++ct) {
                 const float nm = fmaxf(mx[ct], tm[ct]), alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx[ct] - nm);
                 mx[ct] = nm;
-                sum[ct] *= alpha;
+                if constexpr (TERMS == 1) total[ct][0] *= alpha; else sum[ct] *= alpha;
 #pragma unroll
                 for (int j = 0; j < KC; ++j) { o[ct][j][0] *= alpha; o[ct][j][1] *= alpha; }
             }
@@ -292,7 +298,7 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
                 for (int v = 0; v < 4; ++v) {
                     const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[ct][t][v], a.scale2, -base));
                     sc[ct][t][v] = e;
-                    part += e;
+                    if constexpr (TERMS > 1) part += e;
                 }
             sum[ct] += part;
 #pragma unroll
@@ -323,6 +329,10 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
         }
         // ---- products with V
         __builtin_amdgcn_s_setprio(1);
+        if constexpr (TERMS == 1)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+                total[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ONES), __builtin_bit_cast(bf16x8, pf[ct][0]), total[ct], 0, 0, 0);
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
             u32x4 even, odd;
@@ -353,6 +363,7 @@ __global__ __launch_bounds__(64 * NW, (PagesForm<HD, CT, TERMS, PACK, NW>::WAVES
         float t = sum[ct];
         t += __shfl_xor(t, 16, 64);
         t += __shfl_xor(t, 32, 64);
+        if constexpr (TERMS == 1) t = total[ct][0];
         if (g == 0 && group == 0) { mx_sh[wave][ct * W + col] = mx[ct]; sum_sh[wave][ct * W + col] = t; }
     }
     float* rec = nrec == 1 ? nullptr : a.rec + ((((size_t)b * pl.KH + kh) * a.ncg + cg) * a.nsp + sp) * (W * CT) * OS;
@@ -445,6 +456,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 4 : 3) void attn_pages_long_kerne
     }
     f32x4 o[KC][2];
     float mx = -INFINITY, sum = 0.f;
+    f32x4 total = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < KC; ++j) o[j][0] = o[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int tshift = pl.shift - 4, tlast = max(seen - 1, 0) >> 4;
@@ -542,7 +554,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 4 : 3) void attn_pages_long_kerne
         if (__any(m > mx + 8.f)) {
             const float nm = fmaxf(mx, m), alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx - nm);
             mx = nm;
-            sum *= alpha;
+            if constexpr (TERMS == 1) total[0] *= alpha; else sum *= alpha;
 #pragma unroll
             for (int j = 0; j < KC; ++j) { o[j][0] *= alpha; o[j][1] *= alpha; }
         }
@@ -559,7 +571,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 4 : 3) void attn_pages_long_kerne
             for (int v = 0; v < 4; ++v) {
                 const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][v], a.scale2, -base));
                 sc[t][v] = e;
-                part += e;
+                if constexpr (TERMS > 1) part += e;
             }
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
@@ -571,6 +583,10 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 4 : 3) void attn_pages_long_kerne
         }
         sum += part;
         __builtin_amdgcn_s_setprio(1);
+        if constexpr (TERMS == 1)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) total = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ONES), __builtin_bit_cast(bf16x8, pf[s][0]), total, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
             const bf16x8 vf = __builtin_bit_cast(bf16x8, fr[f % AHEAD]);
@@ -583,6 +599,7 @@ __global__ __launch_bounds__(256, TERMS == 1 ? 4 : 3) void attn_pages_long_kerne
     }
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
+    if constexpr (TERMS == 1) sum = total[0];
     if (c >= ncol) return;
     // every lane has eight neighbouring dimensions of its column per chunk: 32 j + 8 g .. + 7
     const int cc = wave * 16 + col;

@@ -124,7 +124,9 @@ def attention(q, K, V, lens, n_new, scale, bf16):
 
     Bound.  A score is off by A = scale sum |q| |k| times: fp32, the three-term q (2^-24); its sum in 32 bits (hd + 4 terms of 2^-24, each
     product exact).  The exponent's argument and exp2 add (|score| + 4) 2^-23.  An error d of all scores moves every weight by at most a
-    factor e^(2 d), 2.1 d while d is small.  Weights: bf16, half a step 2^-8 (fp32, three terms: 2^-24); their sum and the products' L 2^-24; the merges
+    factor e^(2 d), 2.1 d while d is small.  Weights: bf16, half a step 2^-8 (fp32, three terms: 2^-24)
+    each, and bf16 ones are divided by the sum of the rounded weights: with w_i (1 + e_i), |e_i| <= 2^-8, the output is off by
+    sum w_i e_i (v_i - out) to first order, at most 2^-8 (sum w_i |v_i| + |out|); their sum and the products' L 2^-24; the merges
     and the division 64 2^-24.  Output in bf16: half a step of it."""
     rows, H, hd = q.shape
     out, bound = np.zeros((rows, H, hd)), np.zeros((rows, H, hd))
@@ -145,7 +147,7 @@ def attention(q, K, V, lens, n_new, scale, bf16):
                     out[at + i, h] = w @ v
                     d = float((scale * (np.abs(k) @ np.abs(x))).max()) * ((0 if bf16 else H24) + (hd + 4) * H24) + (np.abs(s).max() * 1.5 + 4) * 2 * H24
                     rel = 2.1 * d + (H8 if bf16 else H24) + (see + 64) * H24
-                    bound[at + i, h] = (w @ np.abs(v)) * rel * 1.01 + (H8 * np.abs(out[at + i, h]) * 1.01 if bf16 else 0) + 1e-37
+                    bound[at + i, h] = (w @ np.abs(v)) * rel * 1.01 + (2 * H8 * np.abs(out[at + i, h]) * 1.01 if bf16 else 0) + 1e-37
         at += n
     return out, bound
 
